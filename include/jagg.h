@@ -16,6 +16,16 @@
  *   dit_joint_vjp      Phase 4: grad += sum_rows J(z_row, t_row)^T cot_row
  *   grad_reduce        gradient accumulation and the cosine / norm-ratio reductions
  *
+ * and, for projections whose operands are held in 8 bits and for the trainer's step after the
+ * gradient:
+ *
+ *   jagg_rms_norm_fp8  residual addition, RMS norm, output in 8 bits with scales
+ *   jagg_rms_norm_bwd  its backward pass
+ *   jagg_quantize_fp8  a matrix in 8 bits: groups along rows, along columns, in blocks
+ *   jagg_gemm_fp8      dense products of 8-bit operands, plain and for both gradients
+ *   jagg_grad_norm     the global norm of many gradient tensors
+ *   jagg_grad_clip     gradients times min(1, max_norm / norm)
+ *
  * Conventions shared by every entry point:
  *   - Memory is owned by the caller.  Pointers documented "device" must be device
  *     memory of the current CUDA device; "host" pointers are ordinary host memory.
@@ -75,8 +85,8 @@ int64_t jagg_launch_count(void);
  * adds two event records per launch); jagg_profile_enable(0) stops.  Families, in this
  * order: gemm_tcgen05, gemm_simt, attention_fwd, attention_bwd, ln_gate_bwd,
  * attention_bwd_aux, qk_norm_rope_bwd, colsum, copy_rows, step_signals, grad_reduce,
- * ln_mod_fwd, qk_norm_rope_fwd (step_signals and grad_reduce cover a whole call of the
- * entry point).  jagg_profile_read synchronises the device and fills up to `cap` entries,
+ * ln_mod_fwd, qk_norm_rope_fwd, gemm_fp8, rms_norm_fp8, rms_norm_bwd, quantize_fp8, grad_clip
+ * (step_signals, grad_reduce and the last four cover a whole call of the entry point).  jagg_profile_read synchronises the device and fills up to `cap` entries,
  * one per family: launches, summed device milliseconds, summed algorithmic FLOPs (2 per
  * multiply-add of the products the operation defines) and algorithmic bytes (each input
  * read once, each output written once). */
@@ -321,6 +331,116 @@ int jagg_route(int n_windows, double jagg_frac, const double* cos, double tau,
 int64_t jagg_grad_reduce_workspace_bytes(int64_t P);
 int grad_reduce(const float* a, const float* b, int64_t P, float alpha, float* acc,
                 double* out3, void* ws, size_t ws_bytes, cudaStream_t stream);
+
+/* ------------------------------------------------------------------ 8-bit operands
+ * A matrix [rows, cols] in 8 bits is a row-major array of e4m3 codes with row pitch ldq, and
+ * f32 scales: element (r, c) stands for scale * e4m3(q[r * ldq + c]).  A scale serves a group of
+ * 128 (the last group of a row, a column or a side may be shorter):
+ *   row groups    1 x 128     scale[(c / 128) * lds + r]            lds >= rows
+ *   column groups 128 x 1     scale[(r / 128) * lds + c]            lds >= cols
+ *   blocks        128 x 128   scale[(r / 128) * lds + c / 128]      lds >= ceil(cols / 128)
+ * The library writes scale = max(amax / 448, 2^-126), amax the largest magnitude of the group and
+ * 448 the largest e4m3 value, and q = e4m3(x / scale), rounded to nearest even.  A group of zeros
+ * stands for zeros exactly.  A group that holds a NaN or an infinity stands for NaN throughout.
+ * Codes are read and written inside [rows, cols] only: what lies between cols and ldq is left
+ * alone.  q must be 16-byte aligned with ldq a multiple of 16; scales may have any pitch.
+ * Sides of 0 are allowed: nothing is launched, or an empty sum is written.
+ * JAGG_DTYPE_* arguments name f32 or bf16. */
+
+/* h = round(x + residual) in h_dtype, y = h / sqrt(mean(h^2) + eps) * weight row by row, and y in 8
+ * bits with row groups.  The mean is taken of h as it is stored, so that jagg_rms_norm_bwd, which
+ * reads h, differentiates this function; sums and y are f32.
+ *   x         device [rows, d] x_dtype, row pitch ldx
+ *   residual  device [rows, d] h_dtype, row pitch ldh, or NULL (h = round(x))
+ *   weight    device [d] w_dtype, or NULL (ones)
+ *   h_out     device [rows, d] h_dtype, row pitch ldh, or NULL; may be the residual's buffer
+ *   q, scale  device, row groups of [rows, d]
+ *   rstd      device [rows] f32, 1 / sqrt(mean(h^2) + eps), or NULL
+ * 1 <= d <= 32768.  x, residual and h_out need the alignment of their elements only; with 16-byte
+ * aligned rows and d a multiple of 8 a faster kernel runs. */
+int jagg_rms_norm_fp8(const void* x, int x_dtype, int64_t ldx, const void* residual, int h_dtype, int64_t ldh,
+                      const void* weight, int w_dtype, int64_t rows, int64_t d, float eps, void* h_out, uint8_t* q,
+                      int64_t ldq, float* scale, int64_t lds, float* rstd, cudaStream_t stream);
+
+/* The backward pass of that norm (the 8-bit rounding passes gradients through unchanged).  With
+ * xhat = h rstd and g = dy weight:
+ *   dx      = dh + rstd (g - xhat mean(g xhat))     the gradient of x and of the residual
+ *   dweight = sum over rows of dy xhat              (+= when accumulate != 0)
+ *   dy    device [rows, d] dy_dtype, row pitch lddy   gradient of y
+ *   h     device [rows, d] h_dtype, row pitch ldh     as stored by the forward pass
+ *   dh    device [rows, d] h_dtype, row pitch ldg, or NULL: the gradient that reaches h directly
+ *   dx    device [rows, d] h_dtype, row pitch ldg; may be dh's buffer
+ *   dweight device [d] f32 or NULL; sums over rows are taken in a fixed order
+ *   ws    device workspace of >= jagg_rms_norm_bwd_workspace_bytes(rows, d) bytes (NULL when
+ *         dweight is); nothing in it needs to be zero                                     */
+int64_t jagg_rms_norm_bwd_workspace_bytes(int64_t rows, int64_t d);
+int jagg_rms_norm_bwd(const void* dy, int dy_dtype, int64_t lddy, const void* h, int h_dtype, int64_t ldh,
+                      const void* weight, int w_dtype, const float* rstd, const void* dh, void* dx, int64_t ldg,
+                      int64_t rows, int64_t d, float* dweight, int accumulate, void* ws, size_t ws_bytes,
+                      cudaStream_t stream);
+
+/* x row_mul col_mul (element (r, c) times row_mul[r] and col_mul[c]; NULL: ones) in 8 bits, in any of
+ * the three forms, all from one read of x.  A form whose q is NULL is not written.
+ * With x = h, row_mul = rstd and col_mul = weight the norm's output is formed again, for the
+ * weight gradient (which takes column groups).
+ *   x        device [rows, cols] x_dtype, row pitch ldx
+ *   row_mul  device [rows] f32;  col_mul  device [cols] col_mul_dtype                     */
+typedef struct jagg_fp8_out {
+  uint8_t* q;
+  int64_t ldq;
+  float* scale;
+  int64_t lds;
+} jagg_fp8_out;
+int jagg_quantize_fp8(const void* x, int x_dtype, int64_t ldx, int64_t rows, int64_t cols, const float* row_mul,
+                      const void* col_mul, int col_mul_dtype, const jagg_fp8_out* by_row, const jagg_fp8_out* by_col,
+                      const jagg_fp8_out* by_block, cudaStream_t stream);
+
+/* C[m, n] (+)= sum_k A[m, k] B[n, k] (+ bias[n]) with 8-bit operands:
+ *   A   a_trans = 0: stored [M, K] with row groups; a_trans = 1: stored [K, M] with column groups
+ *   B   b_trans = 0: stored [N, K] with row groups, or blocks (b_block = 1);
+ *       b_trans = 1: stored [K, N] with column groups, or blocks
+ * so a weight [out, in] quantised once in blocks serves the forward product (b_trans = 0) and the
+ * input's gradient (A = dY, b_trans = 1), and dY, X with column groups give the weight's gradient
+ * (a_trans = b_trans = 1, M = out, N = in, K = tokens) without a transposed copy.
+ * Each group of 128 along K is summed by the tensor cores in f32, scaled, and added in f32.  The
+ * product of two scales must be finite.
+ *   C     device [M, N] c_dtype, row pitch ldc, aligned to its elements; accumulate != 0 adds to
+ *         it (f32 only)
+ *   bias  device [N] bias_dtype or NULL                                                  */
+typedef struct jagg_gemm_fp8_desc {
+  int64_t M, N, K;
+  const uint8_t* A;
+  int64_t lda;
+  const float* a_scale;
+  int64_t lda_scale;
+  const uint8_t* B;
+  int64_t ldb;
+  const float* b_scale;
+  int64_t ldb_scale;
+  void* C;
+  int64_t ldc;
+  const void* bias;
+  int32_t a_trans, b_trans, b_block, c_dtype, bias_dtype, accumulate;
+} jagg_gemm_fp8_desc;
+int jagg_gemm_fp8(const jagg_gemm_fp8_desc* desc, cudaStream_t stream);
+
+/* ------------------------------------------------------------------ gradient norm and clipping
+ * Over `count` tensors in device memory (grads: host array of device pointers, numel: host array of
+ * lengths, 0 allowed; dtype of all of them; any alignment of whole elements):
+ *   norm = sqrt(sum of squares over all tensors),  coef = min(1, max_norm / (norm + eps))
+ * The arrays are read before the call returns.  Squares are summed in f32 over a few terms and in f64
+ * beyond (in f64 throughout where they leave f32's range), in a fixed order.
+ * jagg_grad_norm writes norm to norm_out (device f32 [1]).
+ * jagg_grad_clip writes {norm, coef} to norm_out (device f32 [2]) and out[i] = coef grads[i] (NULL: in
+ * place; an out tensor is its gradient's own buffer or does not overlap any gradient).  Where coef
+ * is 1 nothing is written in place.  A NaN or infinite gradient makes the norm that: NaN leaves NaN
+ * in every output, infinity leaves 0 in every finite element and NaN in the infinite ones.
+ *   ws    device workspace of >= jagg_grad_clip_workspace_bytes(count) bytes, 8-byte aligned */
+int64_t jagg_grad_clip_workspace_bytes(int count);
+int jagg_grad_norm(const void* const* grads, const int64_t* numel, int count, int dtype, float* norm_out, void* ws,
+                   size_t ws_bytes, cudaStream_t stream);
+int jagg_grad_clip(void* const* grads, void* const* out, const int64_t* numel, int count, int dtype, double max_norm,
+                   double eps, float* norm_out, void* ws, size_t ws_bytes, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

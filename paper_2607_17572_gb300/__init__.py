@@ -61,6 +61,20 @@ class GemmDesc(ctypes.Structure):
                 ("tile_n", ctypes.c_int32), ("col_sum", ctypes.c_void_p)]
 
 
+class Fp8Out(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("scale", ctypes.c_void_p), ("lds", ctypes.c_int64)]
+
+
+class GemmFp8Desc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("A", ctypes.c_void_p),
+                ("lda", ctypes.c_int64), ("a_scale", ctypes.c_void_p), ("lda_scale", ctypes.c_int64),
+                ("B", ctypes.c_void_p), ("ldb", ctypes.c_int64), ("b_scale", ctypes.c_void_p),
+                ("ldb_scale", ctypes.c_int64), ("C", ctypes.c_void_p), ("ldc", ctypes.c_int64),
+                ("bias", ctypes.c_void_p), ("a_trans", ctypes.c_int32), ("b_trans", ctypes.c_int32),
+                ("b_block", ctypes.c_int32), ("c_dtype", ctypes.c_int32), ("bias_dtype", ctypes.c_int32),
+                ("accumulate", ctypes.c_int32)]
+
+
 class ProfileStat(ctypes.Structure):
     _fields_ = [("family", ctypes.c_char * 32), ("launches", ctypes.c_int64), ("ms", ctypes.c_double),
                 ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
@@ -111,6 +125,17 @@ _SIGNATURES = {
     "jagg_route": (_I, [_I, _D, _P, _D, _P, _P]),
     "jagg_grad_reduce_workspace_bytes": (_I64, [_I64]),
     "grad_reduce": (_I, [_P, _P, _I64, ctypes.c_float, _P, _P, _P, _SZ, _P]),
+    "jagg_rms_norm_fp8": (_I, [_P, _I, _I64, _P, _I, _I64, _P, _I, _I64, _I64, ctypes.c_float, _P, _P, _I64, _P,
+                               _I64, _P, _P]),
+    "jagg_rms_norm_bwd_workspace_bytes": (_I64, [_I64, _I64]),
+    "jagg_rms_norm_bwd": (_I, [_P, _I, _I64, _P, _I, _I64, _P, _I, _P, _P, _P, _I64, _I64, _I64, _P, _I, _P, _SZ,
+                               _P]),
+    "jagg_quantize_fp8": (_I, [_P, _I, _I64, _I64, _I64, _P, _P, _I, ctypes.POINTER(Fp8Out),
+                               ctypes.POINTER(Fp8Out), ctypes.POINTER(Fp8Out), _P]),
+    "jagg_gemm_fp8": (_I, [ctypes.POINTER(GemmFp8Desc), _P]),
+    "jagg_grad_clip_workspace_bytes": (_I64, [_I]),
+    "jagg_grad_norm": (_I, [_P, _P, _I, _I, _P, _P, _SZ, _P]),
+    "jagg_grad_clip": (_I, [_P, _P, _P, _I, _I, _D, _D, _P, _P, _SZ, _P]),
     "jagg_test_gemm": (_I, [ctypes.POINTER(GemmDesc), _P]),
     "jagg_test_gemm_pair": (_I, [ctypes.POINTER(GemmDesc), ctypes.POINTER(GemmDesc), _I, _I, _I, _I, _P]),
     "jagg_test_wait_timeout": (_I, [ctypes.c_ulonglong, _P, _P]),
@@ -390,6 +415,241 @@ def grad_reduce(a, b=None, alpha: float = 1.0, acc=None, out3=None, ws=None, str
                              0 if ws is None else ws.numel(), _stream(stream)), "grad_reduce")
 
 
+# ----------------------------------------------------------------------------- 8-bit operands
+_FP8 = (torch.float8_e4m3fn, torch.uint8)
+_CODE = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+
+
+def _groups(n: int) -> int:
+    return -(-n // 128)
+
+
+def _on(*ts):
+    """The CUDA device that every given tensor lies on."""
+    dev = None
+    for t in ts:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise JaggError("device tensors must be CUDA tensors")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise JaggError(f"tensors on {dev} and {t.device}")
+    return dev
+
+
+def _launch(dev, stream, call):
+    """call(stream handle) with `dev` current, on the given stream or the device's current one."""
+    if stream is not None and stream.device != dev:
+        raise JaggError(f"a stream of {stream.device} for tensors on {dev}")
+    if dev.index == torch.cuda.current_device():
+        return call((stream or torch.cuda.current_stream(dev)).cuda_stream)
+    with torch.cuda.device(dev):
+        return call((stream or torch.cuda.current_stream(dev)).cuda_stream)
+
+
+def _dtype(t, what: str) -> int:
+    if t is None:
+        return DTYPE_F32
+    code = _CODE.get(t.dtype)
+    if code is None:
+        raise JaggError(f"{what} is {t.dtype}: float32 or bfloat16 are taken")
+    return code
+
+
+def _rows(t, shape, what: str) -> int:
+    """Row pitch in elements of a [rows, cols] tensor whose rows are contiguous."""
+    if tuple(t.shape) != tuple(shape):
+        raise JaggError(f"{what} is {tuple(t.shape)}: {tuple(shape)} expected")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise JaggError(f"{what}: the elements of a row must be contiguous")
+    ld = t.stride(0)
+    if t.shape[0] <= 1 or t.shape[1] == 0:  # the stride of a single row says nothing
+        ld = max(ld, t.shape[1])
+    elif ld < t.shape[1]:
+        raise JaggError(f"{what}: rows overlap (pitch {ld} below {t.shape[1]})")
+    return ld
+
+
+def _vector(t, n: int, what: str):
+    if t is not None and (t.shape != (n,) or (n > 1 and t.stride(0) != 1)):
+        raise JaggError(f"{what} is {tuple(t.shape)}: a contiguous vector of {n} expected")
+
+
+def _codes(q, shape, what: str) -> int:
+    if q.dtype not in _FP8:
+        raise JaggError(f"{what} is {q.dtype}: float8_e4m3fn or uint8 expected")
+    ld = _rows(q, shape, what)
+    # a single row's pitch is free: the next multiple of 16
+    return -(-ld // 16) * 16 if shape[0] == 1 else ld
+
+
+def _scales(s, shape, what: str) -> int:
+    if s.dtype != torch.float32:
+        raise JaggError(f"{what} are {s.dtype}: float32 expected")
+    return _rows(s, shape, what)
+
+
+def fp8_buffers(rows: int, cols: int, form: str, device="cuda"):
+    """Codes [rows, cols] (float8_e4m3fn, row pitch a multiple of 16) and scales (f32) of a matrix in
+    8 bits: form "row" (scales [ceil(cols / 128), rows]), "col" ([ceil(rows / 128), cols]) or
+    "block" ([ceil(rows / 128), ceil(cols / 128)])."""
+    shape = {"row": (_groups(cols), rows), "col": (_groups(rows), cols), "block": (_groups(rows), _groups(cols))}[form]
+    q = torch.empty(rows, -(-cols // 16) * 16, dtype=torch.float8_e4m3fn, device=device)[:, :cols]
+    return q, torch.empty(shape, dtype=torch.float32, device=device)
+
+
+def rms_norm_fp8(x, q, scale, residual=None, weight=None, eps: float = 1e-6, h_out=None, rstd=None, stream=None):
+    """h = x + residual, y = h / sqrt(mean(h^2) + eps) * weight, y in 8 bits with row groups
+    (jagg_rms_norm_fp8).  x [rows, d]; q, scale as fp8_buffers(rows, d, "row"); residual and
+    h_out [rows, d] of one dtype and pitch (h_out may be residual); rstd [rows] f32."""
+    dev = _on(x, q, scale, residual, weight, h_out, rstd)
+    rows, d = x.shape
+    held = residual if residual is not None else h_out
+    hd = _dtype(held if held is not None else x, "residual / h_out")
+    ldh = _rows(held, x.shape, "residual / h_out") if held is not None else d
+    if residual is not None and h_out is not None:
+        if h_out.dtype != residual.dtype:
+            raise JaggError("residual and h_out differ in dtype")
+        if _rows(h_out, x.shape, "h_out") != ldh:
+            raise JaggError("residual and h_out differ in row pitch")
+    _vector(weight, d, "weight")
+    _vector(rstd, rows, "rstd")
+    if rstd is not None and rstd.dtype != torch.float32:
+        raise JaggError("rstd must be float32")
+    args = (_ptr(x), _dtype(x, "x"), _rows(x, x.shape, "x"), _ptr(residual), hd, ldh, _ptr(weight),
+            _dtype(weight, "weight"), rows, d, eps, _ptr(h_out), _ptr(q), _codes(q, x.shape, "q"), _ptr(scale),
+            _scales(scale, (_groups(d), rows), "scale"), _ptr(rstd))
+    _check(_launch(dev, stream, lambda s: lib().jagg_rms_norm_fp8(*args, s)), "jagg_rms_norm_fp8")
+
+
+def rms_norm_bwd_workspace_bytes(rows: int, d: int) -> int:
+    return lib().jagg_rms_norm_bwd_workspace_bytes(rows, d)
+
+
+def rms_norm_bwd(dy, h, rstd, dx, weight=None, dh=None, dweight=None, accumulate: bool = False, ws=None,
+                 stream=None):
+    """The norm's backward (jagg_rms_norm_bwd): dx = dh + the gradient through the norm, dweight
+    [d] f32 written or (accumulate) added to.  dh may be dx; ws is needed with dweight."""
+    dev = _on(dy, h, rstd, dx, weight, dh, dweight, ws)
+    rows, d = h.shape
+    if dx.dtype != h.dtype or (dh is not None and dh.dtype != h.dtype):
+        raise JaggError("h, dh and dx must have one dtype")
+    ldg = _rows(dx, h.shape, "dx")
+    if dh is not None and _rows(dh, h.shape, "dh") != ldg:
+        raise JaggError("dh and dx differ in row pitch")
+    for t, n, what in ((weight, d, "weight"), (rstd, rows, "rstd"), (dweight, d, "dweight")):
+        _vector(t, n, what)
+    if rstd.dtype != torch.float32 or (dweight is not None and dweight.dtype != torch.float32):
+        raise JaggError("rstd and dweight must be float32")
+    args = (_ptr(dy), _dtype(dy, "dy"), _rows(dy, h.shape, "dy"), _ptr(h), _dtype(h, "h"), _rows(h, h.shape, "h"),
+            _ptr(weight), _dtype(weight, "weight"), _ptr(rstd), _ptr(dh), _ptr(dx), ldg, rows, d, _ptr(dweight),
+            int(accumulate), _ptr(ws), _bytes(ws))
+    _check(_launch(dev, stream, lambda s: lib().jagg_rms_norm_bwd(*args, s)), "jagg_rms_norm_bwd")
+
+
+def _bytes(ws) -> int:
+    if ws is None:
+        return 0
+    if not ws.is_contiguous():
+        raise JaggError("a workspace must be contiguous")
+    return ws.numel() * ws.element_size()
+
+
+def quantize_fp8(x, row=None, col=None, block=None, row_mul=None, col_mul=None, stream=None):
+    """x (times row_mul[r] col_mul[c]) in 8 bits (jagg_quantize_fp8): each of row, col, block is a
+    pair (q, scale) as fp8_buffers(rows, cols, form) gives, or None; all from one read of x."""
+    forms = {"row": row, "col": col, "block": block}
+    dev = _on(x, row_mul, col_mul, *[t for f in forms.values() if f is not None for t in f])
+    rows, cols = x.shape
+    shapes = {"row": (_groups(cols), rows), "col": (_groups(rows), cols), "block": (_groups(rows), _groups(cols))}
+    outs = []
+    for name, f in forms.items():
+        if f is None:
+            outs.append(None)
+            continue
+        outs.append(Fp8Out(_ptr(f[0]), _codes(f[0], x.shape, name + " codes"), _ptr(f[1]),
+                           _scales(f[1], shapes[name], name + " scales")))
+    _vector(row_mul, rows, "row_mul")
+    _vector(col_mul, cols, "col_mul")
+    if row_mul is not None and row_mul.dtype != torch.float32:
+        raise JaggError("row_mul must be float32")
+    args = (_ptr(x), _dtype(x, "x"), _rows(x, x.shape, "x"), rows, cols, _ptr(row_mul), _ptr(col_mul),
+            _dtype(col_mul, "col_mul"), *[ctypes.byref(o) if o is not None else None for o in outs])
+    _check(_launch(dev, stream, lambda s: lib().jagg_quantize_fp8(*args, s)), "jagg_quantize_fp8")
+
+
+def gemm_fp8(a, a_scale, b, b_scale, c, a_trans: bool = False, b_trans: bool = False, bias=None,
+             accumulate: bool = False, stream=None):
+    """c [M, N] (+)= A B^T (+ bias) of 8-bit operands (jagg_gemm_fp8).  a is [M, K] with row groups,
+    or with a_trans [K, M] with column groups; b is [N, K] with row groups or blocks, or with
+    b_trans [K, N] with column groups or blocks: which, is seen from the shape of b_scale."""
+    dev = _on(a, a_scale, b, b_scale, c, bias)
+    K, M = a.shape if a_trans else a.shape[::-1]
+    N = b.shape[1] if b_trans else b.shape[0]
+    vector = (_groups(K), N)
+    blocks = (_groups(K), _groups(N)) if b_trans else (_groups(N), _groups(K))
+    b_block = tuple(b_scale.shape) != vector
+    _vector(bias, N, "bias")
+    d = GemmFp8Desc(M, N, K, _ptr(a), _codes(a, a.shape, "a"), _ptr(a_scale),
+                    _scales(a_scale, (_groups(K), M), "a_scale"), _ptr(b),
+                    _codes(b, (K, N) if b_trans else (N, K), "b"), _ptr(b_scale),
+                    _scales(b_scale, blocks if b_block else vector, "b_scale"), _ptr(c), _rows(c, (M, N), "c"),
+                    _ptr(bias), int(a_trans), int(b_trans), int(b_block), _dtype(c, "c"), _dtype(bias, "bias"),
+                    int(accumulate))
+    _check(_launch(dev, stream, lambda s: lib().jagg_gemm_fp8(ctypes.byref(d), s)), "jagg_gemm_fp8")
+
+
+# ----------------------------------------------------------------------------- gradient norm and clipping
+def grad_clip_workspace_bytes(count: int) -> int:
+    return lib().jagg_grad_clip_workspace_bytes(count)
+
+
+def _tensor_list(ts, like=None):
+    """Addresses and lengths of contiguous tensors of one dtype and device."""
+    for t in ts:
+        if not t.is_contiguous():
+            raise JaggError("gradients must be contiguous")
+        if t.dtype != ts[0].dtype:
+            raise JaggError("gradients must have one dtype")
+    n = [t.numel() for t in ts]
+    if like is not None and n != like:
+        raise JaggError("gradients and outputs differ in number or length")
+    return (_P * max(len(ts), 1))(*[t.data_ptr() for t in ts]), n
+
+
+def _clip(name, grads, out, norm_out, ws, stream, *limits):
+    grads = list(grads)
+    dev = _on(norm_out, ws, *grads, *(out or ()))
+    if norm_out.dtype != torch.float32 or norm_out.numel() < (2 if limits else 1) or not norm_out.is_contiguous():
+        raise JaggError("norm_out must hold %d contiguous float32" % (2 if limits else 1))
+    ptrs, n = _tensor_list(grads)
+    lens = (_I64 * max(len(n), 1))(*n)
+    args = [ptrs, lens, len(n), _dtype(grads[0], "gradient") if grads else DTYPE_F32, *limits, _ptr(norm_out),
+            _ptr(ws), _bytes(ws)]
+    if limits:
+        outs = None
+        if out is not None:
+            out = list(out)
+            if out and out[0].dtype != grads[0].dtype:
+                raise JaggError("gradients and outputs differ in dtype")
+            outs = _tensor_list(out, n)[0]
+        args.insert(1, outs)
+    _check(_launch(dev, stream, lambda s: getattr(lib(), name)(*args, s)), name)
+
+
+def grad_norm(grads, norm_out, ws, stream=None):
+    """norm_out[0] (f32) = the global 2-norm of the gradient tensors (jagg_grad_norm)."""
+    _clip("jagg_grad_norm", grads, None, norm_out, ws, stream)
+
+
+def grad_clip(grads, max_norm: float, norm_out, ws, out=None, eps: float = 1e-6, stream=None):
+    """Every gradient times coef = min(1, max_norm / (norm + eps)), in place or into `out` (tensors of
+    the same lengths); norm_out (f32 [2]) receives norm and coef (jagg_grad_clip)."""
+    _clip("jagg_grad_clip", grads, out, norm_out, ws, stream, float(max_norm), float(eps))
+
+
 def launch_count() -> int:
     return lib().jagg_launch_count()
 
@@ -400,9 +660,9 @@ def profile_enable(on: bool):
 
 def profile_read() -> dict:
     """{family: {"launches", "ms", "flops", "bytes"}} (synchronises the device)."""
-    arr = (ProfileStat * 16)()
+    arr = (ProfileStat * 32)()
     n = _I()
-    _check(lib().jagg_profile_read(arr, 16, ctypes.byref(n)), "jagg_profile_read")
+    _check(lib().jagg_profile_read(arr, 32, ctypes.byref(n)), "jagg_profile_read")
     return {arr[i].family.decode(): dict(launches=arr[i].launches, ms=arr[i].ms, flops=arr[i].flops,
                                          bytes=arr[i].bytes) for i in range(n.value)}
 

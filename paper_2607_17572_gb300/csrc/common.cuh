@@ -39,6 +39,7 @@ int unit_status_signals(unsigned* v, int clear);
 int unit_status_elementwise(unsigned* v, int clear);
 int unit_status_attention_tc(unsigned* v, int clear);
 int unit_status_testing(unsigned* v, int clear);
+int unit_status_gemm_fp8(unsigned* v, int clear);
 
 __device__ __forceinline__ void set_device_status(unsigned bits) { atomicOr(&g_device_status, bits); }
 
@@ -142,6 +143,11 @@ enum ProfFamily : int {
   PROF_GRAD_REDUCE,
   PROF_LN_FWD,     // LayerNorm + modulation forward
   PROF_QKN_FWD,    // per-head RMSNorm + RoPE forward
+  PROF_GEMM_FP8,   // products of 8-bit operands
+  PROF_NORM_FP8,   // RMS norm with an 8-bit output
+  PROF_NORM_BWD,   // its backward
+  PROF_QUANT_FP8,  // quantisation
+  PROF_GRAD_CLIP,  // gradient norm and clipping
   PROF_FAMILIES
 };
 

@@ -1,0 +1,469 @@
+// Products of 8-bit operands with a scale for each group of 128 along K (include/jagg.h,
+// jagg_gemm_fp8).
+//
+//   C[m, n] = sum_g sa[g, m] sb[g, n] sum_{k in g} A[m, k] B[n, k]
+//
+// The inner sums run on the tensor cores (tcgen05.mma.kind::f8f6f4, f32 accumulators in tensor
+// memory); a k-block is one group, so each accumulator is one inner sum.  The epilogue warps read it
+// back, multiply by the two scales and add to f32 registers while the tensor core works on the next
+// groups in the other accumulators.
+//
+// One CTA holds a tile of 128 rows of one operand ("P", the rows of the accumulator) and up to 128
+// of the other ("Q", its columns).  With few rows of A the weight is P and the tokens are Q, so that the
+// tensor core's 128 rows are all in use and a token tile is as narrow as 16.  A cluster of up to 8
+// CTAs splits K: each sums its k-blocks, the partial tiles meet in shared memory and every CTA
+// joins and stores its part of the tile, in the order of the ranks (no atomics, no workspace).
+//
+// Roles: warp 0 TMA producer, warp 1 MMA issuer, warps 4-7 epilogue (tensor-memory lanes
+// 32 (warp % 4) .. + 31); all warps join and store.
+#include <cuda.h>
+
+#include "fp8.cuh"
+#include "gemm_fp8.cuh"
+#include "ptx.cuh"
+#include "tmap.cuh"
+
+namespace jagg {
+
+int unit_status_gemm_fp8(unsigned* v, int clear) { return read_unit_status(v, clear); }
+
+namespace {
+
+using fp8::GROUP;
+
+constexpr int F_ROWS = 128;                  // P rows of a tile
+constexpr int F_THREADS = 256;
+constexpr int F_TILE = F_ROWS * GROUP;       // bytes of a whole operand tile of a k-block
+constexpr int F_ACCS = 4;                    // accumulators in tensor memory
+constexpr int F_MAX_STAGES = 10;
+constexpr int F_MAX_SPLITS = 8;              // portable cluster size
+constexpr int F_SMEM = 200 * 1024;
+
+template <int NT, bool Q_MN>
+struct FCfg {
+  // MN-major Q rows arrive in whole 128-byte rows (the width of the swizzle), whatever part is used
+  static constexpr int Q_BYTES = Q_MN ? F_TILE : NT * GROUP;
+  static constexpr int STAGE = F_TILE + Q_BYTES;
+  static constexpr int FIT = (F_SMEM - 2048) / STAGE;
+  static constexpr int STAGES = FIT < F_MAX_STAGES ? FIT : F_MAX_STAGES;
+  static constexpr int SMEM = STAGES * STAGE + 1024;
+  static constexpr int COLS = F_ACCS * NT < 32 ? 32 : F_ACCS * NT;  // tensor-memory columns
+};
+
+struct FParams {
+  int P, Q;                // rows of the two operands
+  int tiles_p, k_blocks, splits;
+  const float* ps;         // P's scales
+  int64_t ps_ld, ps_step;
+  const float* qs;
+  int64_t qs_ld, qs_step;
+  int p_block, q_block, p_mn;
+  void* C;
+  int64_t ldc;
+  int c_f32, accumulate, c_vec;
+  const void* bias;
+  int bias_f32;
+};
+struct FMaps {
+  CUtensorMap p, q;
+};
+
+__device__ __forceinline__ void named_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+// SWAP: P is B and Q is A (the tile is C's transpose).
+template <int NT, bool Q_MN, bool SWAP>
+__global__ void __launch_bounds__(F_THREADS, 1) gemm_fp8_kernel(const __grid_constant__ FMaps maps, const FParams p) {
+  using Cfg = FCfg<NT, Q_MN>;
+  extern __shared__ uint8_t smem_f8[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_f8) + 1023) & ~uintptr_t(1023));
+  __shared__ uint64_t full[F_MAX_STAGES], empty[F_MAX_STAGES], tfull[F_ACCS], tempty[F_ACCS], drainbar;
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int abort_flag;
+  __shared__ __align__(16) float qscale[2][NT];
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = p.splits > 1 ? (int)ptx::cluster_ctarank() : 0;
+  const int tile = blockIdx.x / p.splits;
+  const int p0 = (tile % p.tiles_p) * F_ROWS, q0 = (tile / p.tiles_p) * NT;
+  const int kb0 = (int)((long long)p.k_blocks * rank / p.splits);
+  const int kb1 = (int)((long long)p.k_blocks * (rank + 1) / p.splits);
+
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int s = 0; s < Cfg::STAGES; ++s) {
+      ptx::mbar_init(&full[s], 1);
+      ptx::mbar_init(&empty[s], 1);
+    }
+    for (int a = 0; a < F_ACCS; ++a) {
+      ptx::mbar_init(&tfull[a], 1);
+      ptx::mbar_init(&tempty[a], 4);
+    }
+    ptx::mbar_init(&drainbar, 1);
+    ptx::fence_mbar_init();
+    if (p.k_blocks > 0) {
+      ptx::prefetch_tmap(&maps.p);
+      ptx::prefetch_tmap(&maps.q);
+    }
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc(&tmem_slot, Cfg::COLS);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  pdl_wait();
+
+  float acc[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) acc[j] = 0.f;
+
+  if (warp == 0) {
+    if (ptx::elect_one()) {
+      // ---------------- TMA producer
+      int stage = 0;
+      uint32_t phase = 0, issued = 0, issued_parity = 0;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!ptx::mbar_wait(&empty[stage], phase ^ 1)) { abort_flag = 1; break; }
+        uint8_t* sP = smem + stage * Cfg::STAGE;
+        ptx::mbar_arrive_expect_tx(&full[stage], Cfg::STAGE);
+        if (p.p_mn)
+          ptx::tma_load_2d(sP, &maps.p, &full[stage], p0, kb * GROUP);
+        else
+          ptx::tma_load_2d(sP, &maps.p, &full[stage], kb * GROUP, p0);
+        if (Q_MN)
+          ptx::tma_load_2d(sP + F_TILE, &maps.q, &full[stage], q0, kb * GROUP);
+        else
+          ptx::tma_load_2d(sP + F_TILE, &maps.q, &full[stage], kb * GROUP, q0);
+        issued |= 1u << stage;
+        issued_parity = (issued_parity & ~(1u << stage)) | (phase << stage);
+        if (++stage == Cfg::STAGES) { stage = 0; phase ^= 1; }
+      }
+      if (abort_flag)  // after a give-up: loads already issued land before shared memory goes away
+        for (int s = 0; s < Cfg::STAGES; ++s)
+          if (issued & (1u << s)) ptx::mbar_wait(&full[s], (issued_parity >> s) & 1u);
+    }
+  } else if (warp == 1) {
+    if (ptx::elect_one()) {
+      // ---------------- MMA issuer: one accumulator per k-block
+      const uint32_t idesc = ptx::idesc_e4m3(F_ROWS, NT, p.p_mn != 0, Q_MN);
+      // 32 elements of K: 32 bytes inside the swizzled K-major row, or four 1024-byte atoms of
+      // eight MN-major rows
+      const uint64_t p_step = p.p_mn ? 256 : 2, q_step = Q_MN ? 256 : 2;
+      int stage = 0, a = 0;
+      uint32_t phase = 0, a_phase = 0;
+      bool ok = true;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!ptx::mbar_wait(&tempty[a], a_phase ^ 1) || !ptx::mbar_wait(&full[stage], phase)) { ok = false; break; }
+        ptx::tc_fence_after();
+        const uint32_t sP = ptx::smem_u32(smem + stage * Cfg::STAGE);
+        const uint64_t pd = ptx::sdesc_sw128(sP, p.p_mn ? F_TILE : 16, 1024);
+        const uint64_t qd = ptx::sdesc_sw128(sP + F_TILE, Q_MN ? F_TILE : 16, 1024);
+#pragma unroll
+        for (int k = 0; k < GROUP / 32; ++k)
+          ptx::umma_f8(tmem + a * NT, pd + k * p_step, qd + k * q_step, idesc, k > 0 ? 1u : 0u);
+        ptx::umma_commit(&empty[stage]);
+        ptx::umma_commit(&tfull[a]);
+        if (++stage == Cfg::STAGES) { stage = 0; phase ^= 1; }
+        if (++a == F_ACCS) { a = 0; a_phase ^= 1; }
+      }
+      if (!ok) abort_flag = 1;
+      if (abort_flag) {  // products may still be running
+        ptx::umma_commit(&drainbar);
+        ptx::mbar_wait(&drainbar, 0);
+      }
+    }
+  } else if (warp >= 4) {
+    // ---------------- epilogue: thread = P row
+    const int q4 = warp & 3, et = threadIdx.x - 128;
+    const uint32_t trow = tmem + ((uint32_t)(q4 * 32) << 16);
+    const int prow = p0 + et;
+    const float* ps = p.ps + (p.p_block ? (int64_t)(p0 / GROUP) * p.ps_step : (int64_t)prow);
+    const bool p_live = p.p_block || prow < p.P;
+    // vector scales of Q: thread e loads column e's
+    const bool q_vec = !p.q_block;
+    const int qcol = q0 + et;
+    const bool q_live = q_vec ? (et < NT && qcol < p.Q) : true;
+    const float* qs = p.qs + (q_vec ? (int64_t)qcol : (int64_t)(q0 / GROUP) * p.qs_step);
+    auto p_at = [&](int kb) { return kb < kb1 && p_live ? ps[(int64_t)kb * p.ps_ld] : 0.f; };
+    auto q_at = [&](int kb) { return kb < kb1 && q_live ? qs[(int64_t)kb * p.qs_ld] : 0.f; };
+    float pn = p_at(kb0), qn = q_at(kb0);  // of the next k-block
+    int a = 0;
+    uint32_t a_phase = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      const float pv = pn, qv = qn;
+      pn = p_at(kb + 1);
+      qn = q_at(kb + 1);
+      const float* qrow = qscale[kb & 1];
+      if (q_vec) {
+        // written two k-blocks ago, read by everyone before the last barrier
+        if (et < NT) qscale[kb & 1][et] = qv;
+        named_sync(1, 128);
+      }
+      // after a give-up the loop is carried on without data, so that the barriers stay matched
+      const bool ok = __all_sync(0xffffffffu, !abort_flag && ptx::mbar_wait(&tfull[a], a_phase));
+      if (!ok) abort_flag = 1;
+      ptx::tc_fence_after();
+      const float s = pv * (q_vec ? 1.f : qv);
+      const float2 s2 = make_float2(s, s);
+      constexpr int STEP = NT < 32 ? 16 : 32;
+#pragma unroll
+      for (int c = 0; c < NT; c += STEP) {
+        uint32_t r[STEP];
+        if constexpr (STEP == 32)
+          ptx::tmem_ld_32x32b_x32(trow + a * NT + c, r);
+        else
+          ptx::tmem_ld_32x32b_x16(trow + a * NT + c, r);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < STEP; j += 4) {
+          float2 lo = make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
+          float2 hi = make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
+          if (q_vec) {
+            const float4 f = *reinterpret_cast<const float4*>(qrow + c + j);
+            lo = ptx::mul2(lo, make_float2(f.x, f.y));
+            hi = ptx::mul2(hi, make_float2(f.z, f.w));
+          }
+          lo = ptx::fma2(lo, s2, make_float2(acc[c + j], acc[c + j + 1]));
+          hi = ptx::fma2(hi, s2, make_float2(acc[c + j + 2], acc[c + j + 3]));
+          acc[c + j] = lo.x; acc[c + j + 1] = lo.y;
+          acc[c + j + 2] = hi.x; acc[c + j + 3] = hi.y;
+        }
+      }
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&tempty[a]);
+      if (++a == F_ACCS) { a = 0; a_phase ^= 1; }
+    }
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(tmem, Cfg::COLS);
+  }
+  // ---------------- join the splits and store; the operand ring is free (every load has been
+  // consumed by products that have completed)
+  constexpr int PITCH = SWAP ? F_ROWS : NT + 4;  // SWAP: [NT][128]; else [128][NT + 4]
+  static_assert((SWAP ? NT * PITCH : F_ROWS * PITCH) * 4 <= Cfg::STAGES * Cfg::STAGE, "the partial tile fits the ring");
+  float* tilebuf = reinterpret_cast<float*>(smem);
+  if (warp >= 4) {
+    const int et = threadIdx.x - 128;
+    if constexpr (SWAP) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) tilebuf[j * PITCH + et] = acc[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < NT; j += 4)
+        *reinterpret_cast<float4*>(tilebuf + et * PITCH + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
+    }
+  }
+  if (p.splits > 1)
+    ptx::cluster_sync();
+  else
+    __syncthreads();
+  const uint32_t base = ptx::smem_u32(tilebuf);
+  uint32_t peer[F_MAX_SPLITS];
+#pragma unroll
+  for (int c = 0; c < F_MAX_SPLITS; ++c)
+    peer[c] = p.splits > 1 ? ptx::mapa(base, c < p.splits ? c : 0) : base;
+  auto finish = [&](float v, int m, int n) {
+    if (p.bias) v += fp8::load_any(p.bias, p.bias_f32, n);
+    const int64_t at = (int64_t)m * p.ldc + n;
+    if (p.c_f32) {
+      float* c = static_cast<float*>(p.C) + at;
+      *c = p.accumulate ? *c + v : v;
+    } else {
+      static_cast<bf16*>(p.C)[at] = __float2bfloat16_rn(v);
+    }
+  };
+  if constexpr (SWAP) {
+    // columns (tokens) NT rank / splits ..: a warp's lanes store neighbouring n
+    const int j0 = NT * rank / p.splits, j1 = NT * (rank + 1) / p.splits;
+    const int n = p0 + (threadIdx.x & 127);
+    for (int j = j0 + (threadIdx.x >> 7); j < j1; j += 2) {
+      const int m = q0 + j;
+      if (m >= p.Q) break;
+      const uint32_t off = (uint32_t)(j * PITCH + (threadIdx.x & 127)) * 4;
+      float v = 0.f;
+#pragma unroll
+      for (int c = 0; c < F_MAX_SPLITS; ++c)
+        if (c < p.splits) v += ptx::ld_cluster(peer[c] + off);
+      if (n < p.P) finish(v, m, n);
+    }
+  } else {
+    // rows 128 rank / splits ..: a warp's lanes store neighbouring runs of four columns
+    const int r0 = F_ROWS * rank / p.splits, r1 = F_ROWS * (rank + 1) / p.splits;
+    constexpr int RUNS = NT / 4;
+    for (int e = r0 * RUNS + threadIdx.x; e < r1 * RUNS; e += F_THREADS) {
+      const int r = e / RUNS, c4 = (e % RUNS) * 4;
+      const int m = p0 + r, n = q0 + c4;
+      if (m >= p.P || n >= p.Q) continue;
+      const uint32_t off = (uint32_t)(r * PITCH + c4) * 4;
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < F_MAX_SPLITS; ++c)
+        if (c < p.splits) {
+          const float4 f = ptx::ld_cluster_v4(peer[c] + off);
+          v[0] += f.x; v[1] += f.y; v[2] += f.z; v[3] += f.w;
+        }
+      if (p.c_vec && n + 4 <= p.Q) {
+        if (p.bias) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] += fp8::load_any(p.bias, p.bias_f32, n + i);
+        }
+        const int64_t at = (int64_t)m * p.ldc + n;
+        if (p.c_f32) {
+          float4* c = reinterpret_cast<float4*>(static_cast<float*>(p.C) + at);
+          if (p.accumulate) {
+            const float4 o = *c;
+            v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w;
+          }
+          *c = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+          __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
+          *reinterpret_cast<uint2*>(static_cast<bf16*>(p.C) + at) =
+              make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (n + i < p.Q) finish(v[i], m, n + i);
+      }
+    }
+  }
+  if (p.splits > 1) ptx::cluster_sync();  // no CTA leaves while another may read its tile
+}
+
+// ------------------------------------------------------------------ host side
+int operand_map(CUtensorMap* m, const Fp8Operand& o, int64_t rows, int64_t K, int box_rows) {
+  const uint64_t dims[2] = {(uint64_t)(o.mn ? rows : K), (uint64_t)(o.mn ? K : rows)};
+  const uint64_t strides[1] = {(uint64_t)o.ldq};
+  const uint32_t box[2] = {128u, (uint32_t)(o.mn ? GROUP : box_rows)};
+  return encode_tmap_as(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, o.q, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+template <int NT, bool Q_MN, bool SWAP>
+int launch_f8(const GemmFp8Args& g, int splits, cudaStream_t s) {
+  using Cfg = FCfg<NT, Q_MN>;
+  const Fp8Operand &po = SWAP ? g.b : g.a, &qo = SWAP ? g.a : g.b;
+  FParams p{};
+  p.P = (int)(SWAP ? g.N : g.M);
+  p.Q = (int)(SWAP ? g.M : g.N);
+  p.tiles_p = ceil_div(p.P, F_ROWS);
+  p.k_blocks = ceil_div(g.K, GROUP);
+  p.splits = splits;
+  p.ps = po.scale; p.ps_ld = po.ld; p.ps_step = po.row_step; p.p_block = po.block; p.p_mn = po.mn;
+  p.qs = qo.scale; p.qs_ld = qo.ld; p.qs_step = qo.row_step; p.q_block = qo.block;
+  p.C = g.C; p.ldc = g.ldc;
+  p.c_f32 = g.c_dtype == JAGG_DTYPE_F32;
+  p.accumulate = g.accumulate;
+  p.c_vec = p.c_f32 ? fp8::aligned(g.C, 16) && g.ldc % 4 == 0 : fp8::aligned(g.C, 8) && g.ldc % 4 == 0;
+  p.bias = g.bias;
+  p.bias_f32 = g.bias_dtype == JAGG_DTYPE_F32;
+  FMaps maps{};
+  if (g.K > 0) {
+    JAGG_TRY(operand_map(&maps.p, po, p.P, g.K, F_ROWS));
+    JAGG_TRY(operand_map(&maps.q, qo, p.Q, g.K, NT));
+  }
+  auto kernel = gemm_fp8_kernel<NT, Q_MN, SWAP>;
+  static OncePerDevice once;
+  JAGG_CUDA_TRY(allow_smem(once, kernel, Cfg::SMEM));
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = splits;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(p.tiles_p * ceil_div(p.Q, NT) * splits));
+  cfg.blockDim = F_THREADS;
+  cfg.dynamicSmemBytes = Cfg::SMEM;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = splits > 1 ? 2 : 1;
+  JAGG_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, maps, p));
+  JAGG_LAUNCHED();
+  return JAGG_OK;
+}
+
+}  // namespace
+
+int gemm_fp8(const GemmFp8Args& g, cudaStream_t s) {
+  const bool swap = g.M <= 128 && !g.a.mn;
+  const int64_t P = swap ? g.N : g.M, Q = swap ? g.M : g.N;
+  const int nt = swap ? (Q <= 16 ? 16 : Q <= 32 ? 32 : Q <= 64 ? 64 : 128) : 128;
+  const int64_t tiles = (int64_t)ceil_div(P, F_ROWS) * ceil_div(Q, nt);
+  if (tiles > INT32_MAX / F_MAX_SPLITS) {
+    set_last_error("jagg_gemm_fp8: %lld tiles", (long long)tiles);
+    return JAGG_ERR_UNSUPPORTED;
+  }
+  const int kb = ceil_div(g.K, GROUP);
+  int splits = 1;
+  while (splits * 2 <= F_MAX_SPLITS && tiles * splits * 2 <= sm_count() && kb >= 4 * splits) splits *= 2;
+  const int tok = prof_start(s);
+  if (swap) {
+    switch (nt) {
+      case 16: JAGG_TRY((launch_f8<16, false, true>(g, splits, s))); break;
+      case 32: JAGG_TRY((launch_f8<32, false, true>(g, splits, s))); break;
+      case 64: JAGG_TRY((launch_f8<64, false, true>(g, splits, s))); break;
+      default: JAGG_TRY((launch_f8<128, false, true>(g, splits, s))); break;
+    }
+  } else if (g.b.mn) {
+    JAGG_TRY((launch_f8<128, true, false>(g, splits, s)));
+  } else {
+    JAGG_TRY((launch_f8<128, false, false>(g, splits, s)));
+  }
+  prof_stop(tok, s, PROF_GEMM_FP8, 2.0 * g.M * g.N * g.K,
+            (double)g.M * g.K + (double)g.N * g.K + (double)g.M * g.N * (g.c_dtype == JAGG_DTYPE_F32 ? 4 : 2), (int)g.M,
+            (int)g.N, (int)g.K);
+  return JAGG_OK;
+}
+
+}  // namespace jagg
+
+using namespace jagg;
+
+extern "C" int jagg_gemm_fp8(const jagg_gemm_fp8_desc* d, cudaStream_t stream) {
+  const char* who = "jagg_gemm_fp8";
+  JAGG_CHECK_ARG(d, "%s: null descriptor", who);
+  JAGG_CHECK_ARG(d->M >= 0 && d->N >= 0 && d->K >= 0 && d->M < INT32_MAX - 256 && d->N < INT32_MAX - 256 &&
+                     d->K < INT32_MAX - 256,
+                 "%s: M=%lld N=%lld K=%lld outside [0, 2^31 - 257)", who, (long long)d->M, (long long)d->N,
+                 (long long)d->K);
+  JAGG_CHECK_ARG(fp8::is_dtype(d->c_dtype) && fp8::is_dtype(d->bias_dtype), "%s: bad dtype", who);
+  JAGG_CHECK_ARG(!d->accumulate || d->c_dtype == JAGG_DTYPE_F32, "%s: accumulation needs an f32 output", who);
+  if (d->M == 0 || d->N == 0) return JAGG_OK;
+  JAGG_CHECK_ARG(d->C && d->ldc >= d->N && fp8::aligned(d->C, fp8::size_of(d->c_dtype)),
+                 "%s: output null, misaligned, or with a row pitch below N=%lld", who, (long long)d->N);
+  JAGG_CHECK_ARG(fp8::aligned(d->bias, fp8::size_of(d->bias_dtype)), "%s: bias is not aligned to its elements", who);
+  const int64_t kg = (d->K + GROUP - 1) / GROUP, ng = (d->N + GROUP - 1) / GROUP;
+  if (d->K > 0) {
+    const int64_t a_cols = d->a_trans ? d->M : d->K, b_cols = d->b_trans ? d->N : d->K;
+    JAGG_CHECK_ARG(d->A && fp8::aligned(d->A, 16) && d->lda % 16 == 0 && d->lda >= a_cols,
+                   "%s: A needs a 16-byte aligned base and a row pitch that is a multiple of 16 and >= %lld (got %lld)", who,
+                   (long long)a_cols, (long long)d->lda);
+    JAGG_CHECK_ARG(d->B && fp8::aligned(d->B, 16) && d->ldb % 16 == 0 && d->ldb >= b_cols,
+                   "%s: B needs a 16-byte aligned base and a row pitch that is a multiple of 16 and >= %lld (got %lld)", who,
+                   (long long)b_cols, (long long)d->ldb);
+    JAGG_CHECK_ARG(d->a_scale && fp8::aligned(d->a_scale, 4) && d->lda_scale >= d->M,
+                   "%s: A's scales null, misaligned, or with a pitch below M=%lld", who, (long long)d->M);
+    const int64_t b_need = !d->b_block ? d->N : d->b_trans ? ng : kg;
+    JAGG_CHECK_ARG(d->b_scale && fp8::aligned(d->b_scale, 4) && d->ldb_scale >= b_need,
+                   "%s: B's scales null, misaligned, or with a pitch below %lld", who, (long long)b_need);
+  }
+  GemmFp8Args g;
+  g.M = d->M; g.N = d->N; g.K = d->K;
+  g.a.q = d->A; g.a.ldq = d->lda; g.a.scale = d->a_scale; g.a.ld = d->lda_scale; g.a.mn = d->a_trans != 0;
+  g.b.q = d->B; g.b.ldq = d->ldb; g.b.scale = d->b_scale; g.b.mn = d->b_trans != 0; g.b.block = d->b_block != 0;
+  // blocks stored [N, K]: a row of blocks per 128 of N; stored [K, N]: per 128 of K
+  g.b.ld = !g.b.block || g.b.mn ? d->ldb_scale : 1;
+  g.b.row_step = g.b.block ? (g.b.mn ? 1 : d->ldb_scale) : 0;
+  g.C = d->C; g.ldc = d->ldc; g.c_dtype = d->c_dtype;
+  g.bias = d->bias; g.bias_dtype = d->bias_dtype;
+  g.accumulate = d->accumulate != 0;
+  return gemm_fp8(g, stream);
+}

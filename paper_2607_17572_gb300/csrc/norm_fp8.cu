@@ -1,0 +1,661 @@
+// RMS norm with the residual's addition and an 8-bit output, its backward pass, and the
+// quantisation of a matrix in groups of 128 (include/jagg.h, "8-bit operands").
+//
+// All three are bound by device memory: each input is read once, held in registers, and each output
+// written once.  A thread owns runs of eight consecutive elements (16 bytes of bf16), so 16
+// neighbouring lanes hold one group of 128 columns and its largest magnitude is four shuffles.
+#include "fp8.cuh"
+
+namespace jagg {
+namespace {
+
+using namespace fp8;
+
+constexpr int64_t NORM_MAX_D = 32768;
+
+__device__ __forceinline__ float half_warp_amax(float a) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) a = amax(a, __shfl_xor_sync(0xffffffffu, a, o));
+  return a;
+}
+
+struct NormParams {
+  const void* x;
+  int64_t ldx;
+  const void* residual;
+  int64_t ldh;
+  const void* weight;
+  int w_f32;
+  int64_t rows;
+  int d;
+  float eps;
+  void* h_out;
+  uint8_t* q;
+  int64_t ldq;
+  float* scale;
+  int64_t lds;
+  float* rstd;
+};
+
+// The value that h_dtype keeps of v.
+template <typename H>
+__device__ __forceinline__ float kept(float v) {
+  if constexpr (sizeof(H) == 2) return __bfloat162float(__float2bfloat16_rn(v));
+  return v;
+}
+
+// A row for blockDim.x threads (whole warps), blockDim.y rows to a CTA, C runs of eight elements per
+// thread.
+template <typename X, typename H, int C>
+__global__ void __launch_bounds__(1024) rms_norm_fp8_kernel(const NormParams p) {
+  __shared__ float part[32];
+  pdl_wait();
+  const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  const bool live = row < p.rows;
+  const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float v[C][8];
+  float ss = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[c][i] = 0.f;
+    if (live && col < p.d) {
+      load8(static_cast<const X*>(p.x) + row * p.ldx + col, v[c]);
+      if (p.residual) {
+        float r[8];
+        load8(static_cast<const H*>(p.residual) + row * p.ldh + col, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[c][i] += r[i];
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[c][i] = kept<H>(v[c][i]);
+      ss = fmaf(v[c][i], v[c][i], ss);
+    }
+    if (p.h_out && live && col < p.d) store8(static_cast<H*>(p.h_out) + row * p.ldh + col, v[c]);
+  }
+  ss = warp_sum(ss);
+  if (warps > 1) {
+    if (lane == 0) part[threadIdx.y * warps + warp] = ss;
+    __syncthreads();
+    ss = 0.f;
+    for (int w = 0; w < warps; ++w) ss += part[threadIdx.y * warps + w];
+  }
+  const float rstd = 1.f / sqrtf(ss / (float)p.d + p.eps);
+  if (p.rstd && live && threadIdx.x == 0) p.rstd[row] = rstd;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+    const bool in = live && col < p.d;
+    float w[8], a = 0.f;
+    if (p.weight && in) {
+      load8_any(p.weight, p.w_f32, col, w);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = 1.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[c][i] = v[c][i] * rstd * w[i];
+      a = amax(a, v[c][i]);
+    }
+    a = half_warp_amax(in ? a : 0.f);
+    const float s = scale_of(a);
+    if (in) {
+      *reinterpret_cast<uint2*>(p.q + row * p.ldq + col) = pack8(v[c], 1.f / s);
+      if ((lane & 15) == 0) p.scale[(int64_t)(col / GROUP) * p.lds + row] = s;
+    }
+  }
+}
+
+// Any width and alignment: one CTA per row, element by element, the row read twice.
+template <typename X, typename H>
+__global__ void __launch_bounds__(256) rms_norm_fp8_any_kernel(const NormParams p) {
+  __shared__ float part[8];
+  pdl_wait();
+  const int64_t row = blockIdx.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const X* x = static_cast<const X*>(p.x) + row * p.ldx;
+  const H* r = p.residual ? static_cast<const H*>(p.residual) + row * p.ldh : nullptr;
+  H* h = p.h_out ? static_cast<H*>(p.h_out) + row * p.ldh : nullptr;
+  float ss = 0.f;
+  for (int c = threadIdx.x; c < p.d; c += 256) {
+    const float v = kept<H>(ld(x + c) + (r ? ld(r + c) : 0.f));
+    if (h) st(h + c, v);
+    ss = fmaf(v, v, ss);
+  }
+  ss = warp_sum(ss);
+  if (lane == 0) part[warp] = ss;
+  __syncthreads();  // also: h is written before any thread reads it back
+  ss = 0.f;
+  for (int w = 0; w < 8; ++w) ss += part[w];
+  const float rstd = 1.f / sqrtf(ss / (float)p.d + p.eps);
+  if (p.rstd && threadIdx.x == 0) p.rstd[row] = rstd;
+  for (int g0 = warp * GROUP; g0 < p.d; g0 += 8 * GROUP) {
+    float v[4], a = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = g0 + lane + 32 * i;
+      v[i] = 0.f;
+      if (c < p.d) {
+        const float hv = h ? ld(h + c) : kept<H>(ld(x + c) + (r ? ld(r + c) : 0.f));
+        v[i] = hv * rstd * (p.weight ? load_any(p.weight, p.w_f32, c) : 1.f);
+      }
+      a = amax(a, v[i]);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) a = amax(a, __shfl_xor_sync(0xffffffffu, a, o));
+    const float s = scale_of(a), inv = 1.f / s;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = g0 + lane + 32 * i;
+      if (c < p.d) p.q[row * p.ldq + c] = (uint8_t)pack2(v[i] * inv, 0.f);
+    }
+    if (lane == 0) p.scale[(int64_t)(g0 / GROUP) * p.lds + row] = s;
+  }
+}
+
+template <typename X, typename H>
+int launch_norm(const NormParams& p, bool vec, cudaStream_t s) {
+  if (!vec) {
+    JAGG_CUDA_TRY(launch(rms_norm_fp8_any_kernel<X, H>, dim3((unsigned)p.rows), 256, 0, s, p));
+    JAGG_LAUNCHED();
+    return JAGG_OK;
+  }
+  const int chunks = ceil_div(p.d, 256);  // runs of eight for a warp
+  // up to four runs per thread: more rows' loads in flight than with longer runs
+  const int warps = ceil_div(chunks, 4), per = ceil_div(chunks, warps);
+  const int rows = warps >= 4 ? 1 : 4 / warps;
+  const dim3 block(32 * warps, rows), grid((unsigned)((p.rows + rows - 1) / rows));
+  switch (per) {
+    case 1: JAGG_CUDA_TRY(launch(rms_norm_fp8_kernel<X, H, 1>, grid, block, 0, s, p)); break;
+    case 2: JAGG_CUDA_TRY(launch(rms_norm_fp8_kernel<X, H, 2>, grid, block, 0, s, p)); break;
+    case 3: JAGG_CUDA_TRY(launch(rms_norm_fp8_kernel<X, H, 3>, grid, block, 0, s, p)); break;
+    default: JAGG_CUDA_TRY(launch(rms_norm_fp8_kernel<X, H, 4>, grid, block, 0, s, p)); break;
+  }
+  JAGG_LAUNCHED();
+  return JAGG_OK;
+}
+
+// ------------------------------------------------------------------ backward
+struct NormBwdParams {
+  const void* dy;
+  int64_t lddy;
+  const void* h;
+  int64_t ldh;
+  const void* weight;
+  int w_f32;
+  const float* rstd;
+  const void* dh;
+  void* dx;
+  int64_t ldg;
+  int64_t rows;
+  int d;
+  float* part;  // [gridDim.x][d] sums of dy xhat, or null
+};
+
+// Rows in strides over the grid; a thread's columns stay the same, so their weight and their sums
+// over rows live in registers.  One warp per row (blockDim.y rows at a time), or the whole CTA.
+template <typename Y, typename H, int C>
+__global__ void __launch_bounds__(512) rms_norm_bwd_kernel(const NormBwdParams p) {
+  __shared__ float part[2][16];
+  extern __shared__ float cols[];  // [blockDim.y][d] when a CTA takes several rows
+  pdl_wait();
+  const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float w[C][8], dw[C][8];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[c][i] = 1.f, dw[c][i] = 0.f;
+    if (p.weight && col < p.d) load8_any(p.weight, p.w_f32, col, w[c]);
+  }
+  int turn = 0;
+  for (int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; row < p.rows;
+       row += (int64_t)gridDim.x * blockDim.y) {
+    const float rstd = p.rstd[row];
+    float g[C][8], xh[C][8], o[C][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[c][i] = xh[c][i] = o[c][i] = 0.f;
+      if (col < p.d) {
+        load8(static_cast<const Y*>(p.dy) + row * p.lddy + col, g[c]);
+        load8(static_cast<const H*>(p.h) + row * p.ldh + col, xh[c]);
+        if (p.dh) load8(static_cast<const H*>(p.dh) + row * p.ldg + col, o[c]);
+      }
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        xh[c][i] *= rstd;
+        dw[c][i] = fmaf(g[c][i], xh[c][i], dw[c][i]);
+        g[c][i] *= w[c][i];
+        sum = fmaf(g[c][i], xh[c][i], sum);
+      }
+    sum = warp_sum(sum);
+    if (warps > 1) {  // blockDim.y is 1: the whole CTA is at the same row
+      if (lane == 0) part[turn][warp] = sum;
+      __syncthreads();
+      sum = 0.f;
+      for (int k = 0; k < warps; ++k) sum += part[turn][k];
+      turn ^= 1;
+    }
+    const float mean = sum / (float)p.d;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[c][i] = fmaf(rstd, g[c][i] - xh[c][i] * mean, o[c][i]);
+      if (col < p.d) store8(static_cast<H*>(p.dx) + row * p.ldg + col, o[c]);
+    }
+  }
+  if (!p.part) return;
+  float* out = p.part + (int64_t)blockIdx.x * p.d;
+  if (blockDim.y > 1) out = cols + (int64_t)threadIdx.y * p.d;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+    if (col < p.d) store8(out + col, dw[c]);
+  }
+  if (blockDim.y > 1) {
+    __syncthreads();
+    const int t = threadIdx.y * blockDim.x + threadIdx.x, n = blockDim.x * blockDim.y;
+    for (int c = t; c < p.d; c += n) {
+      float s = 0.f;
+      for (int r = 0; r < (int)blockDim.y; ++r) s += cols[(int64_t)r * p.d + c];
+      p.part[(int64_t)blockIdx.x * p.d + c] = s;
+    }
+  }
+}
+
+// Any width and alignment: element by element, the row read twice, sums over rows in shared memory.
+template <typename Y, typename H>
+__global__ void __launch_bounds__(256) rms_norm_bwd_any_kernel(const NormBwdParams p) {
+  __shared__ float part[8];
+  extern __shared__ float cols[];  // [d] when p.part
+  pdl_wait();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (p.part)
+    for (int c = threadIdx.x; c < p.d; c += 256) cols[c] = 0.f;  // a thread's columns are its own throughout
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const Y* dy = static_cast<const Y*>(p.dy) + row * p.lddy;
+    const H* h = static_cast<const H*>(p.h) + row * p.ldh;
+    const H* dh = p.dh ? static_cast<const H*>(p.dh) + row * p.ldg : nullptr;
+    H* dx = static_cast<H*>(p.dx) + row * p.ldg;
+    const float rstd = p.rstd[row];
+    float sum = 0.f;
+    for (int c = threadIdx.x; c < p.d; c += 256) {
+      const float y = ld(dy + c), xh = ld(h + c) * rstd;
+      if (p.part) cols[c] = fmaf(y, xh, cols[c]);
+      sum = fmaf(y * (p.weight ? load_any(p.weight, p.w_f32, c) : 1.f), xh, sum);
+    }
+    sum = warp_sum(sum);
+    __syncthreads();  // the last row's readers are done
+    if (lane == 0) part[warp] = sum;
+    __syncthreads();
+    sum = 0.f;
+    for (int k = 0; k < 8; ++k) sum += part[k];
+    const float mean = sum / (float)p.d;
+    for (int c = threadIdx.x; c < p.d; c += 256) {
+      const float g = ld(dy + c) * (p.weight ? load_any(p.weight, p.w_f32, c) : 1.f), xh = ld(h + c) * rstd;
+      st(dx + c, fmaf(rstd, g - xh * mean, dh ? ld(dh + c) : 0.f));
+    }
+  }
+  if (p.part)
+    for (int c = threadIdx.x; c < p.d; c += 256) p.part[(int64_t)blockIdx.x * p.d + c] = cols[c];
+}
+
+// dweight (+)= the column sums of part [n, d], in order: 32 columns x 8 row lanes per CTA.
+__global__ void __launch_bounds__(256) dweight_kernel(const float* part, int n, int d, float* dweight, int accumulate) {
+  __shared__ float red[8][32];
+  pdl_wait();
+  const int lane = threadIdx.x & 31, r0 = threadIdx.x >> 5;
+  const int c = blockIdx.x * 32 + lane;
+  float s = 0.f;
+  if (c < d) {
+#pragma unroll 8
+    for (int r = r0; r < n; r += 8) s += part[(int64_t)r * d + c];
+  }
+  red[r0][lane] = s;
+  __syncthreads();
+  if (r0 == 0 && c < d) {
+    s = 0.f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) s += red[r][lane];
+    dweight[c] = accumulate ? dweight[c] + s : s;
+  }
+}
+
+constexpr int64_t BWD_VEC_MAX_D = 8192;  // 16 warps of two runs per thread
+constexpr int BWD_MAX_CTAS = 608;  // rows of partial sums in the workspace at most (four per SM)
+
+// CTAs of the backward pass: rows of the workspace.
+int bwd_ctas(int64_t rows, int64_t rows_per_cta) {
+  const int64_t n = (rows + rows_per_cta - 1) / rows_per_cta;
+  return (int)(n < BWD_MAX_CTAS ? n : BWD_MAX_CTAS);
+}
+
+template <typename Y, typename H>
+int launch_norm_bwd(const NormBwdParams& p, bool vec, float* dweight, int accumulate, cudaStream_t s) {
+  int ctas;
+  if (!vec) {
+    ctas = bwd_ctas(p.rows, 1);
+    auto kernel = rms_norm_bwd_any_kernel<Y, H>;
+    static OncePerDevice once;
+    JAGG_CUDA_TRY(allow_smem(once, kernel, (int)NORM_MAX_D * 4));
+    JAGG_CUDA_TRY(launch(kernel, ctas, 256, p.part ? (size_t)p.d * 4 : 0, s, p));
+  } else {
+    const int chunks = ceil_div(p.d, 256);
+    const int warps = ceil_div(chunks, 2), per = ceil_div(chunks, warps);
+    const int rows = warps == 1 ? 8 : 1;
+    ctas = bwd_ctas(p.rows, rows);
+    const dim3 block(32 * warps, rows);
+    const size_t smem = rows > 1 && p.part ? (size_t)rows * p.d * 4 : 0;
+    if (per == 1)
+      JAGG_CUDA_TRY(launch(rms_norm_bwd_kernel<Y, H, 1>, ctas, block, smem, s, p));
+    else
+      JAGG_CUDA_TRY(launch(rms_norm_bwd_kernel<Y, H, 2>, ctas, block, smem, s, p));
+  }
+  JAGG_LAUNCHED();
+  if (p.part) {
+    JAGG_CUDA_TRY(launch(dweight_kernel, ceil_div(p.d, 32), 256, 0, s, (const float*)p.part, ctas, p.d, dweight,
+                         accumulate));
+    JAGG_LAUNCHED();
+  }
+  return JAGG_OK;
+}
+
+// ------------------------------------------------------------------ quantisation
+struct QuantParams {
+  const void* x;
+  int64_t ldx;
+  int64_t rows, cols;
+  const float* row_mul;
+  const void* col_mul;
+  int col_f32;
+  jagg_fp8_out row, col, block;
+};
+
+// A 128 x 128 tile per CTA of 256 threads: thread (c, r) = (t & 15, t >> 4) holds columns 8 c .. + 7 of
+// the rows r, r + 16, .., r + 112, so a row group is one half warp's and a column group is 16
+// threads' eight rows each, joined in shared memory.
+template <typename X, bool VEC>
+__global__ void __launch_bounds__(256) quantize_kernel(const QuantParams p) {
+  __shared__ float peak[16][GROUP];
+  __shared__ float whole[8];
+  pdl_wait();
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
+  const int64_t row0 = (int64_t)blockIdx.y * GROUP, col0 = (int64_t)blockIdx.x * GROUP + 8 * c;
+  const int live = (int)(p.cols - col0 < 0 ? 0 : p.cols - col0 < 8 ? p.cols - col0 : 8);  // columns of this thread
+  float v[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t row = row0 + r + 16 * i;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+    if (row < p.rows) {
+      const X* x = static_cast<const X*>(p.x) + row * p.ldx + col0;
+      if (VEC) {
+        if (live) load8(x, v[i]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < live) v[i][j] = ld(x + j);
+      }
+    }
+  }
+  if (p.row_mul) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = row0 + r + 16 * i;
+      const float m = row < p.rows ? p.row_mul[row] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (row < p.rows && j < live) v[i][j] *= m;
+    }
+  }
+  if (p.col_mul) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j >= live) continue;
+      const float m = load_any(p.col_mul, p.col_f32, col0 + j);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (row0 + r + 16 * i < p.rows) v[i][j] *= m;
+    }
+  }
+  auto put = [&](uint8_t* q, int64_t ldq, int64_t row, const float (&o)[8], float inv) {
+    const uint2 w = pack8(o, inv);
+    uint8_t* at = q + row * ldq + col0;
+    if (VEC) {
+      *reinterpret_cast<uint2*>(at) = w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < live) at[j] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+    }
+  };
+  if (p.row.q) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = row0 + r + 16 * i;
+      float a = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) a = amax(a, v[i][j]);
+      const float s = scale_of(half_warp_amax(a));
+      if (row < p.rows && live) {
+        put(p.row.q, p.row.ldq, row, v[i], 1.f / s);
+        if (c == 0) p.row.scale[(int64_t)blockIdx.x * p.row.lds + row] = s;
+      }
+    }
+  }
+  if (p.col.q) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float a = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a = amax(a, v[i][j]);
+      peak[r][8 * c + j] = a;
+    }
+    __syncthreads();
+    if (threadIdx.x < GROUP) {
+      float a = 0.f;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) a = amax(a, peak[k][threadIdx.x]);
+      const float s = scale_of(a);
+      const int64_t col = (int64_t)blockIdx.x * GROUP + threadIdx.x;
+      if (col < p.cols) p.col.scale[(int64_t)blockIdx.y * p.col.lds + col] = s;
+      peak[0][threadIdx.x] = 1.f / s;  // row 0 of this column has been read by this thread alone
+    }
+    __syncthreads();
+    float inv[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) inv[j] = peak[0][8 * c + j];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = row0 + r + 16 * i;
+      if (row < p.rows && live) {
+        float o[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = v[i][j] * inv[j];
+        put(p.col.q, p.col.ldq, row, o, 1.f);
+      }
+    }
+  }
+  if (p.block.q) {
+    float a = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) a = amax(a, v[i][j]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) a = amax(a, __shfl_xor_sync(0xffffffffu, a, o));
+    if ((threadIdx.x & 31) == 0) whole[threadIdx.x >> 5] = a;
+    __syncthreads();
+    a = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) a = amax(a, whole[k]);
+    const float s = scale_of(a), inv = 1.f / s;
+    if (threadIdx.x == 0) p.block.scale[(int64_t)blockIdx.y * p.block.lds + blockIdx.x] = s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = row0 + r + 16 * i;
+      if (row < p.rows && live) put(p.block.q, p.block.ldq, row, v[i], inv);
+    }
+  }
+}
+
+int check_out(const char* who, const char* form, const jagg_fp8_out* o, int64_t cols, int64_t lds) {
+  JAGG_CHECK_ARG(o->scale, "%s: %s codes without scales", who, form);
+  JAGG_CHECK_ARG(aligned(o->q, 16) && o->ldq % 16 == 0 && o->ldq >= cols,
+                 "%s: %s codes need a 16-byte aligned base and a row pitch that is a multiple of 16 and >= %lld (got %lld)",
+                 who, form, (long long)cols, (long long)o->ldq);
+  JAGG_CHECK_ARG(aligned(o->scale, 4) && o->lds >= lds, "%s: %s scales: pitch %lld below %lld", who, form,
+                 (long long)o->lds, (long long)lds);
+  return JAGG_OK;
+}
+
+}  // namespace
+}  // namespace jagg
+
+using namespace jagg;
+
+extern "C" int jagg_rms_norm_fp8(const void* x, int x_dtype, int64_t ldx, const void* residual, int h_dtype,
+                                 int64_t ldh, const void* weight, int w_dtype, int64_t rows, int64_t d, float eps,
+                                 void* h_out, uint8_t* q, int64_t ldq, float* scale, int64_t lds, float* rstd,
+                                 cudaStream_t stream) {
+  const char* who = "jagg_rms_norm_fp8";
+  JAGG_CHECK_ARG(is_dtype(x_dtype) && is_dtype(h_dtype) && is_dtype(w_dtype), "%s: bad dtype", who);
+  JAGG_CHECK_ARG(rows >= 0 && rows <= INT32_MAX, "%s: rows=%lld outside [0, 2^31)", who, (long long)rows);
+  JAGG_CHECK_ARG(d >= 1, "%s: d=%lld must be positive", who, (long long)d);
+  if (d > NORM_MAX_D) {
+    set_last_error("%s: d=%lld, rows of at most %lld elements are implemented", who, (long long)d, (long long)NORM_MAX_D);
+    return JAGG_ERR_UNSUPPORTED;
+  }
+  if (rows == 0) return JAGG_OK;
+  JAGG_CHECK_ARG(x && q && scale, "%s: null pointer", who);
+  JAGG_CHECK_ARG(ldx >= d && (ldh >= d || (!residual && !h_out)), "%s: a row pitch is below d=%lld", who, (long long)d);
+  const int xs = size_of(x_dtype), hs = size_of(h_dtype), ws = size_of(w_dtype);
+  JAGG_CHECK_ARG(aligned(x, xs) && aligned(residual, hs) && aligned(h_out, hs) && aligned(weight, ws) && aligned(rstd, 4),
+                 "%s: a pointer is not aligned to its elements", who);
+  JAGG_CHECK_ARG(eps >= 0.f, "%s: eps must not be negative", who);
+  const jagg_fp8_out o{q, ldq, scale, lds};
+  JAGG_TRY(check_out(who, "row", &o, d, rows));
+  const NormParams p{x, ldx, residual, ldh, weight, w_dtype == JAGG_DTYPE_F32, rows, (int)d, eps, h_out, q, ldq,
+                     scale, lds, rstd};
+  const bool vec = d % 8 == 0 && aligned(x, 16) && ldx * xs % 16 == 0 && aligned(weight, 16) &&
+                   ((!residual && !h_out) || (aligned(residual, 16) && aligned(h_out, 16) && ldh * hs % 16 == 0));
+  const bool xf = x_dtype == JAGG_DTYPE_F32, hf = h_dtype == JAGG_DTYPE_F32;
+  const int tok = prof_start(stream);
+  if (xf)
+    JAGG_TRY((hf ? launch_norm<float, float>(p, vec, stream) : launch_norm<float, bf16>(p, vec, stream)));
+  else
+    JAGG_TRY((hf ? launch_norm<bf16, float>(p, vec, stream) : launch_norm<bf16, bf16>(p, vec, stream)));
+  prof_stop(tok, stream, PROF_NORM_FP8, 0.0, (double)rows * d * (xs + (residual ? hs : 0) + (h_out ? hs : 0) + 1));
+  return JAGG_OK;
+}
+
+extern "C" int64_t jagg_rms_norm_bwd_workspace_bytes(int64_t rows, int64_t d) {
+  if (rows <= 0 || d <= 0) return 0;
+  return (rows < BWD_MAX_CTAS ? rows : BWD_MAX_CTAS) * d * 4;
+}
+
+extern "C" int jagg_rms_norm_bwd(const void* dy, int dy_dtype, int64_t lddy, const void* h, int h_dtype, int64_t ldh,
+                                 const void* weight, int w_dtype, const float* rstd, const void* dh, void* dx,
+                                 int64_t ldg, int64_t rows, int64_t d, float* dweight, int accumulate, void* ws,
+                                 size_t ws_bytes, cudaStream_t stream) {
+  const char* who = "jagg_rms_norm_bwd";
+  JAGG_CHECK_ARG(is_dtype(dy_dtype) && is_dtype(h_dtype) && is_dtype(w_dtype), "%s: bad dtype", who);
+  JAGG_CHECK_ARG(rows >= 0 && rows <= INT32_MAX, "%s: rows=%lld outside [0, 2^31)", who, (long long)rows);
+  JAGG_CHECK_ARG(d >= 1, "%s: d=%lld must be positive", who, (long long)d);
+  if (d > NORM_MAX_D) {
+    set_last_error("%s: d=%lld, rows of at most %lld elements are implemented", who, (long long)d, (long long)NORM_MAX_D);
+    return JAGG_ERR_UNSUPPORTED;
+  }
+  JAGG_CHECK_ARG(aligned(dweight, 4), "%s: dweight is not aligned to its elements", who);
+  if (rows == 0) {
+    if (dweight && !accumulate) JAGG_CUDA_TRY(cudaMemsetAsync(dweight, 0, d * 4, stream));
+    return JAGG_OK;
+  }
+  JAGG_CHECK_ARG(dy && h && rstd && dx, "%s: null pointer", who);
+  JAGG_CHECK_ARG(lddy >= d && ldh >= d && ldg >= d, "%s: a row pitch is below d=%lld", who, (long long)d);
+  const int ys = size_of(dy_dtype), hs = size_of(h_dtype), wb = size_of(w_dtype);
+  JAGG_CHECK_ARG(aligned(dy, ys) && aligned(h, hs) && aligned(dh, hs) && aligned(dx, hs) && aligned(weight, wb) &&
+                     aligned(rstd, 4),
+                 "%s: a pointer is not aligned to its elements", who);
+  if (dweight) {
+    const int64_t need = jagg_rms_norm_bwd_workspace_bytes(rows, d);
+    if (!ws || (int64_t)ws_bytes < need) {
+      set_last_error("%s: workspace %zu < %lld bytes", who, ws ? ws_bytes : (size_t)0, (long long)need);
+      return JAGG_ERR_WORKSPACE;
+    }
+    JAGG_CHECK_ARG(aligned(ws, 16), "%s: workspace not 16-byte aligned", who);
+  }
+  const NormBwdParams p{dy, lddy, h, ldh, weight, w_dtype == JAGG_DTYPE_F32, rstd, dh, dx, ldg, rows, (int)d,
+                        dweight ? static_cast<float*>(ws) : nullptr};
+  const bool vec = d % 8 == 0 && d <= BWD_VEC_MAX_D && aligned(dy, 16) && lddy * ys % 16 == 0 && aligned(h, 16) && ldh * hs % 16 == 0 &&
+                   aligned(dh, 16) && aligned(dx, 16) && ldg * hs % 16 == 0 && aligned(weight, 16);
+  const bool yf = dy_dtype == JAGG_DTYPE_F32, hf = h_dtype == JAGG_DTYPE_F32;
+  const int tok = prof_start(stream);
+  if (yf)
+    JAGG_TRY((hf ? launch_norm_bwd<float, float>(p, vec, dweight, accumulate, stream)
+                 : launch_norm_bwd<float, bf16>(p, vec, dweight, accumulate, stream)));
+  else
+    JAGG_TRY((hf ? launch_norm_bwd<bf16, float>(p, vec, dweight, accumulate, stream)
+                 : launch_norm_bwd<bf16, bf16>(p, vec, dweight, accumulate, stream)));
+  prof_stop(tok, stream, PROF_NORM_BWD, 0.0, (double)rows * d * (ys + (dh ? 3 : 2) * hs));
+  return JAGG_OK;
+}
+
+extern "C" int jagg_quantize_fp8(const void* x, int x_dtype, int64_t ldx, int64_t rows, int64_t cols,
+                                 const float* row_mul, const void* col_mul, int col_mul_dtype,
+                                 const jagg_fp8_out* by_row, const jagg_fp8_out* by_col, const jagg_fp8_out* by_block,
+                                 cudaStream_t stream) {
+  const char* who = "jagg_quantize_fp8";
+  JAGG_CHECK_ARG(is_dtype(x_dtype) && is_dtype(col_mul_dtype), "%s: bad dtype", who);
+  JAGG_CHECK_ARG(rows >= 0 && rows <= 65535ll * GROUP, "%s: rows=%lld outside [0, %lld]", who, (long long)rows,
+                 65535ll * GROUP);
+  JAGG_CHECK_ARG(cols >= 0 && cols <= INT32_MAX, "%s: cols=%lld outside [0, 2^31)", who, (long long)cols);
+  QuantParams p{x, ldx, rows, cols, row_mul, col_mul, col_mul_dtype == JAGG_DTYPE_F32, {}, {}, {}};
+  const int64_t gr = (rows + GROUP - 1) / GROUP, gc = (cols + GROUP - 1) / GROUP;
+  if (by_row && by_row->q) p.row = *by_row;
+  if (by_col && by_col->q) p.col = *by_col;
+  if (by_block && by_block->q) p.block = *by_block;
+  JAGG_CHECK_ARG(p.row.q || p.col.q || p.block.q || rows == 0 || cols == 0, "%s: no form asked for", who);
+  if (rows == 0 || cols == 0) return JAGG_OK;
+  if (p.row.q) JAGG_TRY(check_out(who, "row", &p.row, cols, rows));
+  if (p.col.q) JAGG_TRY(check_out(who, "column", &p.col, cols, cols));
+  if (p.block.q) JAGG_TRY(check_out(who, "block", &p.block, cols, gc));
+  JAGG_CHECK_ARG(x && ldx >= cols, "%s: null input or row pitch below cols=%lld", who, (long long)cols);
+  const int xs = size_of(x_dtype);
+  JAGG_CHECK_ARG(aligned(x, xs) && aligned(row_mul, 4) && aligned(col_mul, size_of(col_mul_dtype)),
+                 "%s: a pointer is not aligned to its elements", who);
+  const bool vec = cols % 8 == 0 && aligned(x, 16) && ldx * xs % 16 == 0;
+  const dim3 grid((unsigned)gc, (unsigned)gr);
+  const int tok = prof_start(stream);
+  if (x_dtype == JAGG_DTYPE_F32) {
+    if (vec)
+      JAGG_CUDA_TRY(launch(quantize_kernel<float, true>, grid, 256, 0, stream, p));
+    else
+      JAGG_CUDA_TRY(launch(quantize_kernel<float, false>, grid, 256, 0, stream, p));
+  } else {
+    if (vec)
+      JAGG_CUDA_TRY(launch(quantize_kernel<bf16, true>, grid, 256, 0, stream, p));
+    else
+      JAGG_CUDA_TRY(launch(quantize_kernel<bf16, false>, grid, 256, 0, stream, p));
+  }
+  JAGG_LAUNCHED();
+  prof_stop(tok, stream, PROF_QUANT_FP8, 0.0,
+            (double)rows * cols * (xs + (p.row.q != nullptr) + (p.col.q != nullptr) + (p.block.q != nullptr)));
+  return JAGG_OK;
+}

@@ -14,4 +14,8 @@ namespace jagg {
 int encode_tmap(CUtensorMap* m, bool f32, int rank, const void* base, const uint64_t* dims, const uint64_t* strides,
                 const uint32_t* box, CUtensorMapSwizzle swz);
 
+// The same for any element type (strides are bytes).
+int encode_tmap_as(CUtensorMap* m, CUtensorMapDataType type, int rank, const void* base, const uint64_t* dims,
+                   const uint64_t* strides, const uint32_t* box, CUtensorMapSwizzle swz);
+
 }  // namespace jagg
