@@ -343,7 +343,8 @@ int grad_reduce(const float* a, const float* b, int64_t P, float alpha, float* a
  * 448 the largest e4m3 value, and q = e4m3(x / scale), rounded to nearest even.  A group of zeros
  * stands for zeros exactly.  A group that holds a NaN or an infinity stands for NaN throughout.
  * Codes are read and written inside [rows, cols] only: what lies between cols and ldq is left
- * alone.  q must be 16-byte aligned with ldq a multiple of 16; scales may have any pitch.
+ * alone.  q must be 16-byte aligned with ldq a multiple of 16, scales of row and column groups
+ * 16-byte aligned with lds a multiple of 4 (blocks: any).
  * Sides of 0 are allowed: nothing is launched, or an empty sum is written.
  * JAGG_DTYPE_* arguments name f32 or bf16. */
 

@@ -7,7 +7,9 @@ library has not been built, or no CUDA device is present, the calls fail.
 """
 from __future__ import annotations
 
+import array
 import ctypes
+import operator
 import os
 from dataclasses import dataclass
 
@@ -416,112 +418,144 @@ def grad_reduce(a, b=None, alpha: float = 1.0, acc=None, out3=None, ws=None, str
 
 
 # ----------------------------------------------------------------------------- 8-bit operands
+# The checks below look at each tensor once and as briefly as they can: a call on a single token's
+# row lasts 3 us on the GPU, less than the arguments take to pass.
 _FP8 = (torch.float8_e4m3fn, torch.uint8)
 _CODE = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+_F32 = torch.float32
+
+
+# The handle of a device's current stream; building torch's stream object takes 3 us.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _current_stream(dev: int) -> int:
+    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream
 
 
 def _groups(n: int) -> int:
-    return -(-n // 128)
+    return (n + 127) >> 7
 
 
-def _on(*ts):
-    """The CUDA device that every given tensor lies on."""
-    dev = None
-    for t in ts:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise JaggError("device tensors must be CUDA tensors")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise JaggError(f"tensors on {dev} and {t.device}")
-    return dev
+def _elsewhere(what: str, t, dev: int):
+    if t.get_device() < 0 or dev < 0:
+        raise JaggError(f"{what} and its fellows must all be CUDA tensors")
+    raise JaggError(f"{what} lies on device {t.get_device()}, others on {dev}")
 
 
-def _launch(dev, stream, call):
-    """call(stream handle) with `dev` current, on the given stream or the device's current one."""
-    if stream is not None and stream.device != dev:
-        raise JaggError(f"a stream of {stream.device} for tensors on {dev}")
-    if dev.index == torch.cuda.current_device():
-        return call((stream or torch.cuda.current_stream(dev)).cuda_stream)
-    with torch.cuda.device(dev):
-        return call((stream or torch.cuda.current_stream(dev)).cuda_stream)
+def _launch(dev: int, stream, name: str, *args):
+    """The entry point `name` with device `dev` current, on the given stream or the device's current
+    one."""
+    if dev < 0:
+        raise JaggError(f"{name}: device tensors must be CUDA tensors")
+    if stream is not None and stream.device.index != dev:
+        raise JaggError(f"{name}: a stream of {stream.device} for tensors on device {dev}")
+    f = getattr(_lib or lib(), name)
+    handle = _current_stream(dev) if stream is None else stream.cuda_stream
+    if dev == torch.cuda.current_device():
+        status = f(*args, handle)
+    else:
+        with torch.cuda.device(dev):
+            status = f(*args, handle)
+    if status != 0:
+        _check(status, name)
 
 
-def _dtype(t, what: str) -> int:
-    if t is None:
-        return DTYPE_F32
+def _mat(t, dev: int, rows: int, cols: int, what: str):
+    """(address, dtype code, row pitch in elements) of an f32 or bf16 [rows, cols] tensor with contiguous rows."""
     code = _CODE.get(t.dtype)
     if code is None:
         raise JaggError(f"{what} is {t.dtype}: float32 or bfloat16 are taken")
-    return code
+    return t.data_ptr(), code, _pitch(t, dev, rows, cols, what)
 
 
-def _rows(t, shape, what: str) -> int:
-    """Row pitch in elements of a [rows, cols] tensor whose rows are contiguous."""
-    if tuple(t.shape) != tuple(shape):
-        raise JaggError(f"{what} is {tuple(t.shape)}: {tuple(shape)} expected")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+def _pitch(t, dev: int, rows: int, cols: int, what: str) -> int:
+    if t.shape != (rows, cols):
+        raise JaggError(f"{what} is {tuple(t.shape)}: {(rows, cols)} expected")
+    if t.get_device() != dev:
+        _elsewhere(what, t, dev)
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
         raise JaggError(f"{what}: the elements of a row must be contiguous")
-    ld = t.stride(0)
-    if t.shape[0] <= 1 or t.shape[1] == 0:  # the stride of a single row says nothing
-        ld = max(ld, t.shape[1])
-    elif ld < t.shape[1]:
-        raise JaggError(f"{what}: rows overlap (pitch {ld} below {t.shape[1]})")
+    if ld < cols:
+        if rows > 1:
+            raise JaggError(f"{what}: rows overlap (pitch {ld} below {cols})")
+        return cols  # the stride of a single row says nothing
     return ld
 
 
-def _vector(t, n: int, what: str):
-    if t is not None and (t.shape != (n,) or (n > 1 and t.stride(0) != 1)):
+def _vec(t, dev: int, n: int, what: str, f32: bool = False):
+    """(address, dtype code) of a contiguous vector of n, or of None."""
+    if t is None:
+        return None, DTYPE_F32
+    code = _CODE.get(t.dtype)
+    if code is None or (f32 and code != DTYPE_F32):
+        raise JaggError(f"{what} is {t.dtype}: float32{'' if f32 else ' or bfloat16'} expected")
+    if t.shape != (n,) or (n > 1 and t.stride(0) != 1):
         raise JaggError(f"{what} is {tuple(t.shape)}: a contiguous vector of {n} expected")
+    if t.get_device() != dev:
+        _elsewhere(what, t, dev)
+    return t.data_ptr(), code
 
 
-def _codes(q, shape, what: str) -> int:
+def _codes(q, dev: int, rows: int, cols: int, what: str):
+    """(address, row pitch) of 8-bit codes."""
     if q.dtype not in _FP8:
         raise JaggError(f"{what} is {q.dtype}: float8_e4m3fn or uint8 expected")
-    ld = _rows(q, shape, what)
+    ld = _pitch(q, dev, rows, cols, what)
     # a single row's pitch is free: the next multiple of 16
-    return -(-ld // 16) * 16 if shape[0] == 1 else ld
+    return q.data_ptr(), (ld + 15) & ~15 if rows == 1 else ld
 
 
-def _scales(s, shape, what: str) -> int:
-    if s.dtype != torch.float32:
+def _scales(s, dev: int, rows: int, cols: int, what: str):
+    """(address, pitch) of scales; a single row's pitch is free: the next multiple of 4."""
+    if s.dtype != _F32:
         raise JaggError(f"{what} are {s.dtype}: float32 expected")
-    return _rows(s, shape, what)
+    ld = _pitch(s, dev, rows, cols, what)
+    return s.data_ptr(), (ld + 3) & ~3 if rows == 1 else ld
+
+
+def _work(ws, dev: int):
+    """(address, bytes) of a workspace, or of None."""
+    if ws is None:
+        return None, 0
+    if not ws.is_contiguous():
+        raise JaggError("a workspace must be contiguous")
+    if ws.get_device() != dev:
+        _elsewhere("the workspace", ws, dev)
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def fp8_buffers(rows: int, cols: int, form: str, device="cuda"):
-    """Codes [rows, cols] (float8_e4m3fn, row pitch a multiple of 16) and scales (f32) of a matrix in
-    8 bits: form "row" (scales [ceil(cols / 128), rows]), "col" ([ceil(rows / 128), cols]) or
-    "block" ([ceil(rows / 128), ceil(cols / 128)])."""
+    """Codes [rows, cols] (float8_e4m3fn, row pitch a multiple of 16) and scales (f32, row pitch a
+    multiple of 4) of a matrix in 8 bits: form "row" (scales [ceil(cols / 128), rows]), "col"
+    ([ceil(rows / 128), cols]) or "block" ([ceil(rows / 128), ceil(cols / 128)])."""
     shape = {"row": (_groups(cols), rows), "col": (_groups(rows), cols), "block": (_groups(rows), _groups(cols))}[form]
     q = torch.empty(rows, -(-cols // 16) * 16, dtype=torch.float8_e4m3fn, device=device)[:, :cols]
-    return q, torch.empty(shape, dtype=torch.float32, device=device)
+    return q, torch.empty(shape[0], -(-shape[1] // 4) * 4, device=device)[:, :shape[1]]
 
 
 def rms_norm_fp8(x, q, scale, residual=None, weight=None, eps: float = 1e-6, h_out=None, rstd=None, stream=None):
     """h = x + residual, y = h / sqrt(mean(h^2) + eps) * weight, y in 8 bits with row groups
     (jagg_rms_norm_fp8).  x [rows, d]; q, scale as fp8_buffers(rows, d, "row"); residual and
-    h_out [rows, d] of one dtype and pitch (h_out may be residual); rstd [rows] f32."""
-    dev = _on(x, q, scale, residual, weight, h_out, rstd)
+    h_out [rows, d] of one dtype and pitch (h_out may be residual); rstd [rows] f32.  Without either,
+    h is x."""
+    dev = x.get_device()
     rows, d = x.shape
-    held = residual if residual is not None else h_out
-    hd = _dtype(held if held is not None else x, "residual / h_out")
-    ldh = _rows(held, x.shape, "residual / h_out") if held is not None else d
-    if residual is not None and h_out is not None:
-        if h_out.dtype != residual.dtype:
-            raise JaggError("residual and h_out differ in dtype")
-        if _rows(h_out, x.shape, "h_out") != ldh:
-            raise JaggError("residual and h_out differ in row pitch")
-    _vector(weight, d, "weight")
-    _vector(rstd, rows, "rstd")
-    if rstd is not None and rstd.dtype != torch.float32:
-        raise JaggError("rstd must be float32")
-    args = (_ptr(x), _dtype(x, "x"), _rows(x, x.shape, "x"), _ptr(residual), hd, ldh, _ptr(weight),
-            _dtype(weight, "weight"), rows, d, eps, _ptr(h_out), _ptr(q), _codes(q, x.shape, "q"), _ptr(scale),
-            _scales(scale, (_groups(d), rows), "scale"), _ptr(rstd))
-    _check(_launch(dev, stream, lambda s: lib().jagg_rms_norm_fp8(*args, s)), "jagg_rms_norm_fp8")
+    xp, xd, ldx = _mat(x, dev, rows, d, "x")
+    rp, hp, hd, ldh = None, None, xd, d
+    if h_out is not None:
+        hp, hd, ldh = _mat(h_out, dev, rows, d, "h_out")
+    if residual is not None:
+        rp, rd, ldr = _mat(residual, dev, rows, d, "residual")
+        if hp is not None and (rd != hd or ldr != ldh):
+            raise JaggError("residual and h_out differ in dtype or row pitch")
+        hd, ldh = rd, ldr
+    wp, wd = _vec(weight, dev, d, "weight")
+    qp, ldq = _codes(q, dev, rows, d, "q")
+    sp, lds = _scales(scale, dev, _groups(d), rows, "scale")
+    _launch(dev, stream, "jagg_rms_norm_fp8", xp, xd, ldx, rp, hd, ldh, wp, wd, rows, d, eps, hp, qp, ldq, sp, lds,
+            _vec(rstd, dev, rows, "rstd", True)[0])
 
 
 def rms_norm_bwd_workspace_bytes(rows: int, d: int) -> int:
@@ -532,52 +566,41 @@ def rms_norm_bwd(dy, h, rstd, dx, weight=None, dh=None, dweight=None, accumulate
                  stream=None):
     """The norm's backward (jagg_rms_norm_bwd): dx = dh + the gradient through the norm, dweight
     [d] f32 written or (accumulate) added to.  dh may be dx; ws is needed with dweight."""
-    dev = _on(dy, h, rstd, dx, weight, dh, dweight, ws)
+    dev = h.get_device()
     rows, d = h.shape
-    if dx.dtype != h.dtype or (dh is not None and dh.dtype != h.dtype):
-        raise JaggError("h, dh and dx must have one dtype")
-    ldg = _rows(dx, h.shape, "dx")
-    if dh is not None and _rows(dh, h.shape, "dh") != ldg:
-        raise JaggError("dh and dx differ in row pitch")
-    for t, n, what in ((weight, d, "weight"), (rstd, rows, "rstd"), (dweight, d, "dweight")):
-        _vector(t, n, what)
-    if rstd.dtype != torch.float32 or (dweight is not None and dweight.dtype != torch.float32):
-        raise JaggError("rstd and dweight must be float32")
-    args = (_ptr(dy), _dtype(dy, "dy"), _rows(dy, h.shape, "dy"), _ptr(h), _dtype(h, "h"), _rows(h, h.shape, "h"),
-            _ptr(weight), _dtype(weight, "weight"), _ptr(rstd), _ptr(dh), _ptr(dx), ldg, rows, d, _ptr(dweight),
-            int(accumulate), _ptr(ws), _bytes(ws))
-    _check(_launch(dev, stream, lambda s: lib().jagg_rms_norm_bwd(*args, s)), "jagg_rms_norm_bwd")
+    hp, hd, ldh = _mat(h, dev, rows, d, "h")
+    yp, yd, ldy = _mat(dy, dev, rows, d, "dy")
+    xp, xd, ldg = _mat(dx, dev, rows, d, "dx")
+    gp = None
+    if xd != hd:
+        raise JaggError("h and dx must have one dtype")
+    if dh is not None:
+        gp, gd, ldd = _mat(dh, dev, rows, d, "dh")
+        if gd != xd or ldd != ldg:
+            raise JaggError("dh and dx differ in dtype or row pitch")
+    wp, wd = _vec(weight, dev, d, "weight")
+    _launch(dev, stream, "jagg_rms_norm_bwd", yp, yd, ldy, hp, hd, ldh, wp, wd, _vec(rstd, dev, rows, "rstd", True)[0],
+            gp, xp, ldg, rows, d, _vec(dweight, dev, d, "dweight", True)[0], 1 if accumulate else 0, *_work(ws, dev))
 
 
-def _bytes(ws) -> int:
-    if ws is None:
-        return 0
-    if not ws.is_contiguous():
-        raise JaggError("a workspace must be contiguous")
-    return ws.numel() * ws.element_size()
+def _out(form, dev, rows, cols, s_rows, s_cols, what):
+    if form is None:
+        return None
+    q, scale = form
+    return Fp8Out(*_codes(q, dev, rows, cols, what + " codes"), *_scales(scale, dev, s_rows, s_cols, what + " scales"))
 
 
 def quantize_fp8(x, row=None, col=None, block=None, row_mul=None, col_mul=None, stream=None):
     """x (times row_mul[r] col_mul[c]) in 8 bits (jagg_quantize_fp8): each of row, col, block is a
     pair (q, scale) as fp8_buffers(rows, cols, form) gives, or None; all from one read of x."""
-    forms = {"row": row, "col": col, "block": block}
-    dev = _on(x, row_mul, col_mul, *[t for f in forms.values() if f is not None for t in f])
+    dev = x.get_device()
     rows, cols = x.shape
-    shapes = {"row": (_groups(cols), rows), "col": (_groups(rows), cols), "block": (_groups(rows), _groups(cols))}
-    outs = []
-    for name, f in forms.items():
-        if f is None:
-            outs.append(None)
-            continue
-        outs.append(Fp8Out(_ptr(f[0]), _codes(f[0], x.shape, name + " codes"), _ptr(f[1]),
-                           _scales(f[1], shapes[name], name + " scales")))
-    _vector(row_mul, rows, "row_mul")
-    _vector(col_mul, cols, "col_mul")
-    if row_mul is not None and row_mul.dtype != torch.float32:
-        raise JaggError("row_mul must be float32")
-    args = (_ptr(x), _dtype(x, "x"), _rows(x, x.shape, "x"), rows, cols, _ptr(row_mul), _ptr(col_mul),
-            _dtype(col_mul, "col_mul"), *[ctypes.byref(o) if o is not None else None for o in outs])
-    _check(_launch(dev, stream, lambda s: lib().jagg_quantize_fp8(*args, s)), "jagg_quantize_fp8")
+    gr, gc = _groups(rows), _groups(cols)
+    xp, xd, ldx = _mat(x, dev, rows, cols, "x")
+    mp, md = _vec(col_mul, dev, cols, "col_mul")
+    _launch(dev, stream, "jagg_quantize_fp8", xp, xd, ldx, rows, cols, _vec(row_mul, dev, rows, "row_mul", True)[0], mp,
+            md, _out(row, dev, rows, cols, gc, rows, "row"), _out(col, dev, rows, cols, gr, cols, "column"),
+            _out(block, dev, rows, cols, gr, gc, "block"))
 
 
 def gemm_fp8(a, a_scale, b, b_scale, c, a_trans: bool = False, b_trans: bool = False, bias=None,
@@ -585,20 +608,25 @@ def gemm_fp8(a, a_scale, b, b_scale, c, a_trans: bool = False, b_trans: bool = F
     """c [M, N] (+)= A B^T (+ bias) of 8-bit operands (jagg_gemm_fp8).  a is [M, K] with row groups,
     or with a_trans [K, M] with column groups; b is [N, K] with row groups or blocks, or with
     b_trans [K, N] with column groups or blocks: which, is seen from the shape of b_scale."""
-    dev = _on(a, a_scale, b, b_scale, c, bias)
-    K, M = a.shape if a_trans else a.shape[::-1]
-    N = b.shape[1] if b_trans else b.shape[0]
-    vector = (_groups(K), N)
-    blocks = (_groups(K), _groups(N)) if b_trans else (_groups(N), _groups(K))
-    b_block = tuple(b_scale.shape) != vector
-    _vector(bias, N, "bias")
-    d = GemmFp8Desc(M, N, K, _ptr(a), _codes(a, a.shape, "a"), _ptr(a_scale),
-                    _scales(a_scale, (_groups(K), M), "a_scale"), _ptr(b),
-                    _codes(b, (K, N) if b_trans else (N, K), "b"), _ptr(b_scale),
-                    _scales(b_scale, blocks if b_block else vector, "b_scale"), _ptr(c), _rows(c, (M, N), "c"),
-                    _ptr(bias), int(a_trans), int(b_trans), int(b_block), _dtype(c, "c"), _dtype(bias, "bias"),
-                    int(accumulate))
-    _check(_launch(dev, stream, lambda s: lib().jagg_gemm_fp8(ctypes.byref(d), s)), "jagg_gemm_fp8")
+    dev = c.get_device()
+    M, N = c.shape
+    K = a.shape[0] if a_trans else a.shape[1]
+    gk = _groups(K)
+    ap, lda = _codes(a, dev, K, M, "a") if a_trans else _codes(a, dev, M, K, "a")
+    bp, ldb = _codes(b, dev, K, N, "b") if b_trans else _codes(b, dev, N, K, "b")
+    block = b_scale.shape != (gk, N)
+    if not block:
+        sp, lds = _scales(b_scale, dev, gk, N, "b_scale")
+    elif b_trans:
+        sp, lds = _scales(b_scale, dev, gk, _groups(N), "b_scale")
+    else:
+        sp, lds = _scales(b_scale, dev, _groups(N), gk, "b_scale")
+    cp, cd, ldc = _mat(c, dev, M, N, "c")
+    d = GemmFp8Desc(M, N, K, ap, lda, *_scales(a_scale, dev, gk, M, "a_scale"), bp, ldb, sp, lds, cp, ldc, None,
+                    a_trans, b_trans, block, cd, DTYPE_F32, accumulate)
+    if bias is not None:
+        d.bias, d.bias_dtype = _vec(bias, dev, N, "bias")
+    _launch(dev, stream, "jagg_gemm_fp8", d)
 
 
 # ----------------------------------------------------------------------------- gradient norm and clipping
@@ -606,48 +634,49 @@ def grad_clip_workspace_bytes(count: int) -> int:
     return lib().jagg_grad_clip_workspace_bytes(count)
 
 
-def _tensor_list(ts, like=None):
-    """Addresses and lengths of contiguous tensors of one dtype and device."""
-    for t in ts:
-        if not t.is_contiguous():
-            raise JaggError("gradients must be contiguous")
-        if t.dtype != ts[0].dtype:
-            raise JaggError("gradients must have one dtype")
-    n = [t.numel() for t in ts]
+_dtype_of = operator.attrgetter("dtype")
+
+
+def _tensor_list(ts, dev: int, dtype, like=None):
+    """Addresses and lengths of contiguous tensors of one dtype and device, as arrays of 64-bit integers."""
+    T = torch.Tensor
+    if set(map(T.get_device, ts)) - {dev}:
+        raise JaggError(f"gradients and norm_out must all be CUDA tensors on one device ({dev})")
+    if set(map(_dtype_of, ts)) - {dtype}:
+        raise JaggError("gradients and their outputs must have one dtype")
+    if not all(map(T.is_contiguous, ts)):
+        raise JaggError("gradients must be contiguous")
+    n = array.array("q", map(T.numel, ts))
     if like is not None and n != like:
         raise JaggError("gradients and outputs differ in number or length")
-    return (_P * max(len(ts), 1))(*[t.data_ptr() for t in ts]), n
+    return array.array("Q", map(T.data_ptr, ts)), n
 
 
-def _clip(name, grads, out, norm_out, ws, stream, *limits):
+def _clip(name, grads, norm_out, ws, stream, values, out=None, limits=()):
     grads = list(grads)
-    dev = _on(norm_out, ws, *grads, *(out or ()))
-    if norm_out.dtype != torch.float32 or norm_out.numel() < (2 if limits else 1) or not norm_out.is_contiguous():
-        raise JaggError("norm_out must hold %d contiguous float32" % (2 if limits else 1))
-    ptrs, n = _tensor_list(grads)
-    lens = (_I64 * max(len(n), 1))(*n)
-    args = [ptrs, lens, len(n), _dtype(grads[0], "gradient") if grads else DTYPE_F32, *limits, _ptr(norm_out),
-            _ptr(ws), _bytes(ws)]
+    dev = norm_out.get_device()
+    dtype = grads[0].dtype if grads else _F32
+    if dtype not in _CODE:
+        raise JaggError(f"gradients are {dtype}: float32 or bfloat16 are taken")
+    if norm_out.dtype != _F32 or norm_out.numel() < values or not norm_out.is_contiguous():
+        raise JaggError(f"norm_out must hold {values} contiguous float32")
+    ptrs, n = _tensor_list(grads, dev, dtype)
+    args = [ptrs.buffer_info()[0], n.buffer_info()[0], len(n), _CODE[dtype], *limits]
     if limits:
-        outs = None
-        if out is not None:
-            out = list(out)
-            if out and out[0].dtype != grads[0].dtype:
-                raise JaggError("gradients and outputs differ in dtype")
-            outs = _tensor_list(out, n)[0]
-        args.insert(1, outs)
-    _check(_launch(dev, stream, lambda s: getattr(lib(), name)(*args, s)), name)
+        outs = _tensor_list(list(out), dev, dtype, n)[0] if out is not None else None
+        args.insert(1, outs.buffer_info()[0] if out is not None else None)
+    _launch(dev, stream, name, *args, norm_out.data_ptr(), *_work(ws, dev))
 
 
 def grad_norm(grads, norm_out, ws, stream=None):
     """norm_out[0] (f32) = the global 2-norm of the gradient tensors (jagg_grad_norm)."""
-    _clip("jagg_grad_norm", grads, None, norm_out, ws, stream)
+    _clip("jagg_grad_norm", grads, norm_out, ws, stream, 1)
 
 
 def grad_clip(grads, max_norm: float, norm_out, ws, out=None, eps: float = 1e-6, stream=None):
     """Every gradient times coef = min(1, max_norm / (norm + eps)), in place or into `out` (tensors of
     the same lengths); norm_out (f32 [2]) receives norm and coef (jagg_grad_clip)."""
-    _clip("jagg_grad_clip", grads, out, norm_out, ws, stream, float(max_norm), float(eps))
+    _clip("jagg_grad_clip", grads, norm_out, ws, stream, 2, out, (float(max_norm), float(eps)))
 
 
 def launch_count() -> int:

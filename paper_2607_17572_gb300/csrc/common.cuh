@@ -40,6 +40,7 @@ int unit_status_elementwise(unsigned* v, int clear);
 int unit_status_attention_tc(unsigned* v, int clear);
 int unit_status_testing(unsigned* v, int clear);
 int unit_status_gemm_fp8(unsigned* v, int clear);
+int unit_status_gemm_fp8_pair(unsigned* v, int clear);
 
 __device__ __forceinline__ void set_device_status(unsigned bits) { atomicOr(&g_device_status, bits); }
 

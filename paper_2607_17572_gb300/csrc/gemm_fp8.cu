@@ -1,5 +1,5 @@
 // Products of 8-bit operands with a scale for each group of 128 along K (include/jagg.h,
-// jagg_gemm_fp8).
+// jagg_gemm_fp8): the kernel of one CTA per tile, the choice of kernel, and the entry point.
 //
 //   C[m, n] = sum_g sa[g, m] sb[g, n] sum_{k in g} A[m, k] B[n, k]
 //
@@ -14,14 +14,15 @@
 // CTAs splits K: each sums its k-blocks, the partial tiles meet in shared memory and every CTA
 // joins and stores its part of the tile, in the order of the ranks (no atomics, no workspace).
 //
-// Roles: warp 0 TMA producer, warp 1 MMA issuer, warps 4-7 epilogue (tensor-memory lanes
-// 32 (warp % 4) .. + 31); all warps join and store.
-#include <cuda.h>
+// Vector scales arrive by TMA beside the operands, in a ring of slots that outlives the operand
+// stages by the accumulators in flight; block scales are read 32 k-blocks at a time, one per lane.
+//
+// Roles: warp 0 TMA producer, warp 1 MMA issuer, warps 4 and up the epilogue (tensor-memory lanes
+// 32 (warp % 4) .. + 31, 64 or fewer columns); all warps join and store.
+#include <atomic>
+#include <cmath>
 
-#include "fp8.cuh"
 #include "gemm_fp8.cuh"
-#include "ptx.cuh"
-#include "tmap.cuh"
 
 namespace jagg {
 
@@ -32,7 +33,6 @@ namespace {
 using fp8::GROUP;
 
 constexpr int F_ROWS = 128;                  // P rows of a tile
-constexpr int F_THREADS = 256;
 constexpr int F_TILE = F_ROWS * GROUP;       // bytes of a whole operand tile of a k-block
 constexpr int F_ACCS = 4;                    // accumulators in tensor memory
 constexpr int F_MAX_STAGES = 10;
@@ -44,20 +44,24 @@ struct FCfg {
   // MN-major Q rows arrive in whole 128-byte rows (the width of the swizzle), whatever part is used
   static constexpr int Q_BYTES = Q_MN ? F_TILE : NT * GROUP;
   static constexpr int STAGE = F_TILE + Q_BYTES;
-  static constexpr int FIT = (F_SMEM - 2048) / STAGE;
+  static constexpr int FIT = F_SMEM / STAGE;
   static constexpr int STAGES = FIT < F_MAX_STAGES ? FIT : F_MAX_STAGES;
   static constexpr int SMEM = STAGES * STAGE + 1024;
   static constexpr int COLS = F_ACCS * NT < 32 ? 32 : F_ACCS * NT;  // tensor-memory columns
+  static constexpr int CW = NT < 64 ? NT : NT / 2;                  // columns of an epilogue warp
+  static constexpr int EW = 4 * (NT / CW);                          // epilogue warps
+  static constexpr int THREADS = 128 + 32 * EW;
+  // A slot is written for k-block i once the products of i - STAGES are done; those were issued
+  // after the epilogue had finished with k-block i - STAGES - F_ACCS.
+  static constexpr int SLOTS = STAGES + F_ACCS;
 };
 
 struct FParams {
   int P, Q;                // rows of the two operands
   int tiles_p, k_blocks, splits;
-  const float* ps;         // P's scales
-  int64_t ps_ld, ps_step;
-  const float* qs;
-  int64_t qs_ld, qs_step;
-  int p_block, q_block, p_mn;
+  const float* block;      // block scales of P or Q: value (r / 128, g) at r / 128 * block_step + g * block_ld
+  int64_t block_ld, block_step;
+  int p_block, p_mn;
   void* C;
   int64_t ldc;
   int c_f32, accumulate, c_vec;
@@ -65,23 +69,22 @@ struct FParams {
   int bias_f32;
 };
 struct FMaps {
-  CUtensorMap p, q;
+  CUtensorMap p, q, ps, qs;  // operands, their vector scales
 };
 
-__device__ __forceinline__ void named_sync(int id, int threads) {
-  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
-}
-
-// SWAP: P is B and Q is A (the tile is C's transpose).
-template <int NT, bool Q_MN, bool SWAP>
-__global__ void __launch_bounds__(F_THREADS, 1) gemm_fp8_kernel(const __grid_constant__ FMaps maps, const FParams p) {
+// SWAP: P is B and Q is A (the tile is C's transpose).  QVEC: Q has a scale per row, else per block.
+template <int NT, bool Q_MN, bool SWAP, bool QVEC>
+__global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
+    gemm_fp8_kernel(const __grid_constant__ FMaps maps, const FParams p) {
   using Cfg = FCfg<NT, Q_MN>;
+  constexpr int CW = Cfg::CW;
   extern __shared__ uint8_t smem_f8[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_f8) + 1023) & ~uintptr_t(1023));
   __shared__ uint64_t full[F_MAX_STAGES], empty[F_MAX_STAGES], tfull[F_ACCS], tempty[F_ACCS], drainbar;
+  __shared__ uint64_t sfull[Cfg::SLOTS];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
-  __shared__ __align__(16) float qscale[2][NT];
+  __shared__ __align__(128) float pscale[Cfg::SLOTS][F_ROWS], qscale[Cfg::SLOTS][NT < 32 ? 32 : NT];
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = p.splits > 1 ? (int)ptx::cluster_ctarank() : 0;
@@ -98,13 +101,16 @@ __global__ void __launch_bounds__(F_THREADS, 1) gemm_fp8_kernel(const __grid_con
     }
     for (int a = 0; a < F_ACCS; ++a) {
       ptx::mbar_init(&tfull[a], 1);
-      ptx::mbar_init(&tempty[a], 4);
+      ptx::mbar_init(&tempty[a], Cfg::EW);
     }
+    for (int i = 0; i < Cfg::SLOTS; ++i) ptx::mbar_init(&sfull[i], 1);
     ptx::mbar_init(&drainbar, 1);
     ptx::fence_mbar_init();
     if (p.k_blocks > 0) {
       ptx::prefetch_tmap(&maps.p);
       ptx::prefetch_tmap(&maps.q);
+      if (!p.p_block) ptx::prefetch_tmap(&maps.ps);
+      if (QVEC) ptx::prefetch_tmap(&maps.qs);
     }
   }
   if (warp == 1) {
@@ -117,15 +123,16 @@ __global__ void __launch_bounds__(F_THREADS, 1) gemm_fp8_kernel(const __grid_con
   const uint32_t tmem = tmem_slot;
   pdl_wait();
 
-  float acc[NT];
+  float acc[CW];
 #pragma unroll
-  for (int j = 0; j < NT; ++j) acc[j] = 0.f;
+  for (int j = 0; j < CW; ++j) acc[j] = 0.f;
 
   if (warp == 0) {
     if (ptx::elect_one()) {
       // ---------------- TMA producer
-      int stage = 0;
+      int stage = 0, slot = 0;
       uint32_t phase = 0, issued = 0, issued_parity = 0;
+      uint32_t s_phase = 0, s_issued = 0, s_parity = 0;
       for (int kb = kb0; kb < kb1; ++kb) {
         if (!ptx::mbar_wait(&empty[stage], phase ^ 1)) { abort_flag = 1; break; }
         uint8_t* sP = smem + stage * Cfg::STAGE;
@@ -138,13 +145,22 @@ __global__ void __launch_bounds__(F_THREADS, 1) gemm_fp8_kernel(const __grid_con
           ptx::tma_load_2d(sP + F_TILE, &maps.q, &full[stage], q0, kb * GROUP);
         else
           ptx::tma_load_2d(sP + F_TILE, &maps.q, &full[stage], kb * GROUP, q0);
+        ptx::mbar_arrive_expect_tx(&sfull[slot], (p.p_block ? 0 : F_ROWS * 4) + (QVEC ? NT * 4 : 0));
+        if (!p.p_block) ptx::tma_load_2d(pscale[slot], &maps.ps, &sfull[slot], p0, kb);
+        if (QVEC) ptx::tma_load_2d(qscale[slot], &maps.qs, &sfull[slot], q0, kb);
+        s_issued |= 1u << slot;
+        s_parity = (s_parity & ~(1u << slot)) | (s_phase << slot);
+        if (++slot == Cfg::SLOTS) { slot = 0; s_phase ^= 1; }
         issued |= 1u << stage;
         issued_parity = (issued_parity & ~(1u << stage)) | (phase << stage);
         if (++stage == Cfg::STAGES) { stage = 0; phase ^= 1; }
       }
-      if (abort_flag)  // after a give-up: loads already issued land before shared memory goes away
+      if (abort_flag) {  // after a give-up: loads already issued land before shared memory goes away
         for (int s = 0; s < Cfg::STAGES; ++s)
           if (issued & (1u << s)) ptx::mbar_wait(&full[s], (issued_parity >> s) & 1u);
+        for (int s = 0; s < Cfg::SLOTS; ++s)
+          if (s_issued & (1u << s)) ptx::mbar_wait(&sfull[s], (s_parity >> s) & 1u);
+      }
     }
   } else if (warp == 1) {
     if (ptx::elect_one()) {
@@ -177,66 +193,36 @@ __global__ void __launch_bounds__(F_THREADS, 1) gemm_fp8_kernel(const __grid_con
       }
     }
   } else if (warp >= 4) {
-    // ---------------- epilogue: thread = P row
-    const int q4 = warp & 3, et = threadIdx.x - 128;
-    const uint32_t trow = tmem + ((uint32_t)(q4 * 32) << 16);
-    const int prow = p0 + et;
-    const float* ps = p.ps + (p.p_block ? (int64_t)(p0 / GROUP) * p.ps_step : (int64_t)prow);
-    const bool p_live = p.p_block || prow < p.P;
-    // vector scales of Q: thread e loads column e's
-    const bool q_vec = !p.q_block;
-    const int qcol = q0 + et;
-    const bool q_live = q_vec ? (et < NT && qcol < p.Q) : true;
-    const float* qs = p.qs + (q_vec ? (int64_t)qcol : (int64_t)(q0 / GROUP) * p.qs_step);
-    auto p_at = [&](int kb) { return kb < kb1 && p_live ? ps[(int64_t)kb * p.ps_ld] : 0.f; };
-    auto q_at = [&](int kb) { return kb < kb1 && q_live ? qs[(int64_t)kb * p.qs_ld] : 0.f; };
-    float pn = p_at(kb0), qn = q_at(kb0);  // of the next k-block
-    int a = 0;
-    uint32_t a_phase = 0;
+    // ---------------- epilogue: thread = P row, CW columns of Q
+    const int q4 = warp & 3, c0 = ((warp - 4) >> 2) * CW;
+    const int row = q4 * 32 + lane;
+    const uint32_t t0 = tmem + ((uint32_t)(q4 * 32) << 16) + c0;
+    // block scales of 32 k-blocks, one per lane, and of the 32 after them
+    const bool block = p.p_block || !QVEC;
+    const float* bs = p.block + (int64_t)((p.p_block ? p0 : q0) / GROUP) * p.block_step;
+    auto block_at = [&](int kb) { return block && kb < kb1 ? bs[(int64_t)kb * p.block_ld] : 1.f; };
+    float bcur = block_at(kb0 + lane), bnext = block_at(kb0 + 32 + lane);
+    int a = 0, slot = 0;
+    uint32_t a_phase = 0, s_phase = 0;
     for (int kb = kb0; kb < kb1; ++kb) {
-      const float pv = pn, qv = qn;
-      pn = p_at(kb + 1);
-      qn = q_at(kb + 1);
-      const float* qrow = qscale[kb & 1];
-      if (q_vec) {
-        // written two k-blocks ago, read by everyone before the last barrier
-        if (et < NT) qscale[kb & 1][et] = qv;
-        named_sync(1, 128);
+      const int at = (kb - kb0) & 31;
+      if (at == 0 && kb > kb0) {
+        bcur = bnext;
+        bnext = block_at(kb + 32 + lane);
       }
-      // after a give-up the loop is carried on without data, so that the barriers stay matched
-      const bool ok = __all_sync(0xffffffffu, !abort_flag && ptx::mbar_wait(&tfull[a], a_phase));
-      if (!ok) abort_flag = 1;
+      float s = __shfl_sync(0xffffffffu, bcur, at);
+      bool ok = !abort_flag && ptx::mbar_wait(&sfull[slot], s_phase);
+      if (!p.p_block) s *= pscale[slot][row];
+      ok = ok && ptx::mbar_wait(&tfull[a], a_phase);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) { abort_flag = 1; break; }
       ptx::tc_fence_after();
-      const float s = pv * (q_vec ? 1.f : qv);
-      const float2 s2 = make_float2(s, s);
-      constexpr int STEP = NT < 32 ? 16 : 32;
-#pragma unroll
-      for (int c = 0; c < NT; c += STEP) {
-        uint32_t r[STEP];
-        if constexpr (STEP == 32)
-          ptx::tmem_ld_32x32b_x32(trow + a * NT + c, r);
-        else
-          ptx::tmem_ld_32x32b_x16(trow + a * NT + c, r);
-        ptx::tmem_ld_wait();
-#pragma unroll
-        for (int j = 0; j < STEP; j += 4) {
-          float2 lo = make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1]));
-          float2 hi = make_float2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
-          if (q_vec) {
-            const float4 f = *reinterpret_cast<const float4*>(qrow + c + j);
-            lo = ptx::mul2(lo, make_float2(f.x, f.y));
-            hi = ptx::mul2(hi, make_float2(f.z, f.w));
-          }
-          lo = ptx::fma2(lo, s2, make_float2(acc[c + j], acc[c + j + 1]));
-          hi = ptx::fma2(hi, s2, make_float2(acc[c + j + 2], acc[c + j + 3]));
-          acc[c + j] = lo.x; acc[c + j + 1] = lo.y;
-          acc[c + j + 2] = hi.x; acc[c + j + 3] = hi.y;
-        }
-      }
+      fp8::scaled_add<CW, QVEC, (CW < 32 ? 16 : 32)>(acc, t0 + a * NT, s, ptx::smem_u32(qscale[slot] + c0));
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&tempty[a]);
       if (++a == F_ACCS) { a = 0; a_phase ^= 1; }
+      if (++slot == Cfg::SLOTS) { slot = 0; s_phase ^= 1; }
     }
   }
   ptx::tc_fence_before();
@@ -251,14 +237,15 @@ __global__ void __launch_bounds__(F_THREADS, 1) gemm_fp8_kernel(const __grid_con
   static_assert((SWAP ? NT * PITCH : F_ROWS * PITCH) * 4 <= Cfg::STAGES * Cfg::STAGE, "the partial tile fits the ring");
   float* tilebuf = reinterpret_cast<float*>(smem);
   if (warp >= 4) {
-    const int et = threadIdx.x - 128;
-    if constexpr (SWAP) {
+    const int c0 = ((warp - 4) >> 2) * CW, row = (warp & 3) * 32 + lane;
 #pragma unroll
-      for (int j = 0; j < NT; ++j) tilebuf[j * PITCH + et] = acc[j];
-    } else {
-#pragma unroll
-      for (int j = 0; j < NT; j += 4)
-        *reinterpret_cast<float4*>(tilebuf + et * PITCH + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
+    for (int j = 0; j < CW; j += 4) {
+      if constexpr (SWAP) {
+        float* at = tilebuf + (c0 + j) * PITCH + row;
+        at[0] = acc[j]; at[PITCH] = acc[j + 1]; at[2 * PITCH] = acc[j + 2]; at[3 * PITCH] = acc[j + 3];
+      } else {
+        *reinterpret_cast<float4*>(tilebuf + row * PITCH + c0 + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
+      }
     }
   }
   if (p.splits > 1)
@@ -284,7 +271,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) gemm_fp8_kernel(const __grid_con
     // columns (tokens) NT rank / splits ..: a warp's lanes store neighbouring n
     const int j0 = NT * rank / p.splits, j1 = NT * (rank + 1) / p.splits;
     const int n = p0 + (threadIdx.x & 127);
-    for (int j = j0 + (threadIdx.x >> 7); j < j1; j += 2) {
+    for (int j = j0 + (threadIdx.x >> 7); j < j1; j += Cfg::THREADS / 128) {
       const int m = q0 + j;
       if (m >= p.Q) break;
       const uint32_t off = (uint32_t)(j * PITCH + (threadIdx.x & 127)) * 4;
@@ -298,7 +285,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) gemm_fp8_kernel(const __grid_con
     // rows 128 rank / splits ..: a warp's lanes store neighbouring runs of four columns
     const int r0 = F_ROWS * rank / p.splits, r1 = F_ROWS * (rank + 1) / p.splits;
     constexpr int RUNS = NT / 4;
-    for (int e = r0 * RUNS + threadIdx.x; e < r1 * RUNS; e += F_THREADS) {
+    for (int e = r0 * RUNS + threadIdx.x; e < r1 * RUNS; e += Cfg::THREADS) {
       const int r = e / RUNS, c4 = (e % RUNS) * 4;
       const int m = p0 + r, n = q0 + c4;
       if (m >= p.P || n >= p.Q) continue;
@@ -339,14 +326,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) gemm_fp8_kernel(const __grid_con
 }
 
 // ------------------------------------------------------------------ host side
-int operand_map(CUtensorMap* m, const Fp8Operand& o, int64_t rows, int64_t K, int box_rows) {
-  const uint64_t dims[2] = {(uint64_t)(o.mn ? rows : K), (uint64_t)(o.mn ? K : rows)};
-  const uint64_t strides[1] = {(uint64_t)o.ldq};
-  const uint32_t box[2] = {128u, (uint32_t)(o.mn ? GROUP : box_rows)};
-  return encode_tmap_as(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, o.q, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
-}
-
-template <int NT, bool Q_MN, bool SWAP>
+template <int NT, bool Q_MN, bool SWAP, bool QVEC>
 int launch_f8(const GemmFp8Args& g, int splits, cudaStream_t s) {
   using Cfg = FCfg<NT, Q_MN>;
   const Fp8Operand &po = SWAP ? g.b : g.a, &qo = SWAP ? g.a : g.b;
@@ -356,8 +336,9 @@ int launch_f8(const GemmFp8Args& g, int splits, cudaStream_t s) {
   p.tiles_p = ceil_div(p.P, F_ROWS);
   p.k_blocks = ceil_div(g.K, GROUP);
   p.splits = splits;
-  p.ps = po.scale; p.ps_ld = po.ld; p.ps_step = po.row_step; p.p_block = po.block; p.p_mn = po.mn;
-  p.qs = qo.scale; p.qs_ld = qo.ld; p.qs_step = qo.row_step; p.q_block = qo.block;
+  const Fp8Operand& bo = po.block ? po : qo;
+  p.block = bo.scale; p.block_ld = bo.ld; p.block_step = bo.row_step;
+  p.p_block = po.block; p.p_mn = po.mn;
   p.C = g.C; p.ldc = g.ldc;
   p.c_f32 = g.c_dtype == JAGG_DTYPE_F32;
   p.accumulate = g.accumulate;
@@ -366,10 +347,12 @@ int launch_f8(const GemmFp8Args& g, int splits, cudaStream_t s) {
   p.bias_f32 = g.bias_dtype == JAGG_DTYPE_F32;
   FMaps maps{};
   if (g.K > 0) {
-    JAGG_TRY(operand_map(&maps.p, po, p.P, g.K, F_ROWS));
-    JAGG_TRY(operand_map(&maps.q, qo, p.Q, g.K, NT));
+    JAGG_TRY(fp8_operand_map(&maps.p, po, p.P, g.K, F_ROWS));
+    JAGG_TRY(fp8_operand_map(&maps.q, qo, p.Q, g.K, NT));
+    if (!po.block) JAGG_TRY(fp8_scale_map(&maps.ps, po, p.P, g.K, F_ROWS, 1));
+    if (QVEC) JAGG_TRY(fp8_scale_map(&maps.qs, qo, p.Q, g.K, NT, 1));
   }
-  auto kernel = gemm_fp8_kernel<NT, Q_MN, SWAP>;
+  auto kernel = gemm_fp8_kernel<NT, Q_MN, SWAP, QVEC>;
   static OncePerDevice once;
   JAGG_CUDA_TRY(allow_smem(once, kernel, Cfg::SMEM));
   cudaLaunchAttribute attr[2] = {};
@@ -380,7 +363,7 @@ int launch_f8(const GemmFp8Args& g, int splits, cudaStream_t s) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(p.tiles_p * ceil_div(p.Q, NT) * splits));
-  cfg.blockDim = F_THREADS;
+  cfg.blockDim = Cfg::THREADS;
   cfg.dynamicSmemBytes = Cfg::SMEM;
   cfg.stream = s;
   cfg.attrs = attr;
@@ -390,33 +373,116 @@ int launch_f8(const GemmFp8Args& g, int splits, cudaStream_t s) {
   return JAGG_OK;
 }
 
+// How a product is computed: by CTA pairs in tiles of `pair` columns (0: by single CTAs, whose tile has
+// `nt` rows of Q, K split over clusters of `splits`).
+struct Plan {
+  int pair, nt, splits;
+  bool swap;
+};
+
+// Microseconds that a k-block takes, by kernel and tile, and what a tile and a launch take besides;
+// measured on 4096 x 4096 weights with 128 to 8192 rows, and on weight gradients of that size.  B's
+// vector scales cost a multiplication per element more than block scales.
+constexpr double US_LAUNCH = 2.8, US_TILE_ONE = 1.5, US_TILE_PAIR = 2.0, US_JOIN = 1.0;
+double us_one(int nt, bool qvec) { return nt <= 16 ? 0.15 : nt == 32 ? 0.22 : nt == 64 ? 0.4 : qvec ? 0.66 : 0.47; }
+double us_pair(int bn, bool qvec) { return bn == 256 ? (qvec ? 0.78 : 0.46) : qvec ? 0.53 : 0.33; }
+
+// CTAs that run at one time in clusters of n: a cluster has to fit into the SMs of one GPC, so that up
+// to an eighth of the machine stays idle (18 tiles split 8 ways, 144 CTAs, take two turns: 15.6 us,
+// against 6.9 split 4 ways).  Asked once per size; all instances take an SM each.
+int cluster_ctas(int n, int* ctas) {
+  static std::atomic<int> known[F_MAX_SPLITS + 1];
+  *ctas = known[n].load(std::memory_order_relaxed);
+  if (*ctas > 0) return JAGG_OK;
+  auto kernel = gemm_fp8_kernel<128, false, false, false>;
+  using Cfg = FCfg<128, false>;
+  static OncePerDevice once;
+  JAGG_CUDA_TRY(allow_smem(once, kernel, Cfg::SMEM));
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = n;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(n * sm_count());
+  cfg.blockDim = Cfg::THREADS;
+  cfg.dynamicSmemBytes = Cfg::SMEM;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  int clusters = 0;
+  JAGG_CUDA_TRY(cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg));
+  *ctas = clusters > 0 ? clusters * n : n;
+  known[n].store(*ctas, std::memory_order_relaxed);
+  return JAGG_OK;
+}
+
+int plan_of(const GemmFp8Args& g, Plan* plan) {
+  const int kb = ceil_div(g.K, GROUP), sms = sm_count();
+  int room[F_MAX_SPLITS + 1] = {0, sms};
+  for (int s = 2; s <= F_MAX_SPLITS; ++s) JAGG_TRY(cluster_ctas(s, &room[s]));
+  Plan& best = *plan;
+  double least = 0.0;
+  auto offer = [&](const Plan& p, double us) {
+    if (least == 0.0 || us < least) {
+      least = us;
+      best = p;
+    }
+  };
+  auto tiles = [](int64_t rows, int64_t cols, int tr, int tc) {
+    return (double)((rows + tr - 1) / tr) * (double)((cols + tc - 1) / tc);
+  };
+  auto one = [&](bool swap, int nt) {
+    const double t = swap ? tiles(g.N, g.M, F_ROWS, nt) : tiles(g.M, g.N, F_ROWS, nt);
+    const bool qvec = swap || !g.b.block;
+    for (int s = 1; s <= F_MAX_SPLITS && (s == 1 || s <= kb); ++s)
+      offer({0, nt, s, swap}, US_LAUNCH + ceil(t * s / room[s]) * (ceil_div(kb, s) * us_one(nt, qvec) + US_TILE_ONE) +
+                                  (s > 1 ? US_JOIN : 0.0));
+  };
+  one(false, 128);
+  // few rows of A: as many columns of an accumulator as there are tokens (an MN-major A arrives in
+  // whole 128-byte rows, so there is nothing to gain)
+  if (!g.a.mn && g.M <= 64) one(true, g.M <= 16 ? 16 : g.M <= 32 ? 32 : 64);
+  if (g.K > 0)
+    for (int bn : {256, 128})
+      offer({bn, 0, 1, false}, US_LAUNCH + ceil(tiles(g.M, g.N, 256, bn) / (sms / 2)) *
+                                               (kb * us_pair(bn, !g.b.block) + US_TILE_PAIR));
+  return JAGG_OK;
+}
+
+int run_plan(const GemmFp8Args& g, const Plan& p, cudaStream_t s) {
+  if (p.pair) return gemm_fp8_pair(g, p.pair, s);
+  if (p.swap) {
+    if (p.nt == 16) return launch_f8<16, false, true, true>(g, p.splits, s);
+    if (p.nt == 32) return launch_f8<32, false, true, true>(g, p.splits, s);
+    return launch_f8<64, false, true, true>(g, p.splits, s);
+  }
+  if (g.b.mn)
+    return g.b.block ? launch_f8<128, true, false, false>(g, p.splits, s)
+                     : launch_f8<128, true, false, true>(g, p.splits, s);
+  return g.b.block ? launch_f8<128, false, false, false>(g, p.splits, s)
+                   : launch_f8<128, false, false, true>(g, p.splits, s);
+}
+
 }  // namespace
 
+int fp8_operand_map(CUtensorMap* m, const Fp8Operand& o, int64_t rows, int64_t K, int box_rows) {
+  const uint64_t dims[2] = {(uint64_t)(o.mn ? rows : K), (uint64_t)(o.mn ? K : rows)};
+  const uint64_t strides[1] = {(uint64_t)o.ldq};
+  const uint32_t box[2] = {128u, (uint32_t)(o.mn ? GROUP : box_rows)};
+  return encode_tmap_as(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, o.q, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+int fp8_scale_map(CUtensorMap* m, const Fp8Operand& o, int64_t rows, int64_t K, int box_rows, int box_groups) {
+  const uint64_t dims[2] = {(uint64_t)rows, (uint64_t)((K + GROUP - 1) / GROUP)};
+  const uint64_t strides[1] = {(uint64_t)o.ld * 4};
+  const uint32_t box[2] = {(uint32_t)box_rows, (uint32_t)box_groups};
+  return encode_tmap(m, true, 2, o.scale, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
 int gemm_fp8(const GemmFp8Args& g, cudaStream_t s) {
-  const bool swap = g.M <= 128 && !g.a.mn;
-  const int64_t P = swap ? g.N : g.M, Q = swap ? g.M : g.N;
-  const int nt = swap ? (Q <= 16 ? 16 : Q <= 32 ? 32 : Q <= 64 ? 64 : 128) : 128;
-  const int64_t tiles = (int64_t)ceil_div(P, F_ROWS) * ceil_div(Q, nt);
-  if (tiles > INT32_MAX / F_MAX_SPLITS) {
-    set_last_error("jagg_gemm_fp8: %lld tiles", (long long)tiles);
-    return JAGG_ERR_UNSUPPORTED;
-  }
-  const int kb = ceil_div(g.K, GROUP);
-  int splits = 1;
-  while (splits * 2 <= F_MAX_SPLITS && tiles * splits * 2 <= sm_count() && kb >= 4 * splits) splits *= 2;
   const int tok = prof_start(s);
-  if (swap) {
-    switch (nt) {
-      case 16: JAGG_TRY((launch_f8<16, false, true>(g, splits, s))); break;
-      case 32: JAGG_TRY((launch_f8<32, false, true>(g, splits, s))); break;
-      case 64: JAGG_TRY((launch_f8<64, false, true>(g, splits, s))); break;
-      default: JAGG_TRY((launch_f8<128, false, true>(g, splits, s))); break;
-    }
-  } else if (g.b.mn) {
-    JAGG_TRY((launch_f8<128, true, false>(g, splits, s)));
-  } else {
-    JAGG_TRY((launch_f8<128, false, false>(g, splits, s)));
-  }
+  Plan p;
+  JAGG_TRY(plan_of(g, &p));
+  JAGG_TRY(run_plan(g, p, s));
   prof_stop(tok, s, PROF_GEMM_FP8, 2.0 * g.M * g.N * g.K,
             (double)g.M * g.K + (double)g.N * g.K + (double)g.M * g.N * (g.c_dtype == JAGG_DTYPE_F32 ? 4 : 2), (int)g.M,
             (int)g.N, (int)g.K);
@@ -434,6 +500,10 @@ extern "C" int jagg_gemm_fp8(const jagg_gemm_fp8_desc* d, cudaStream_t stream) {
                      d->K < INT32_MAX - 256,
                  "%s: M=%lld N=%lld K=%lld outside [0, 2^31 - 257)", who, (long long)d->M, (long long)d->N,
                  (long long)d->K);
+  if ((d->M + 127) / 128 * ((d->N + 127) / 128) > INT32_MAX / F_MAX_SPLITS) {
+    set_last_error("%s: an output of %lld x %lld is not implemented", who, (long long)d->M, (long long)d->N);
+    return JAGG_ERR_UNSUPPORTED;
+  }
   JAGG_CHECK_ARG(fp8::is_dtype(d->c_dtype) && fp8::is_dtype(d->bias_dtype), "%s: bad dtype", who);
   JAGG_CHECK_ARG(!d->accumulate || d->c_dtype == JAGG_DTYPE_F32, "%s: accumulation needs an f32 output", who);
   if (d->M == 0 || d->N == 0) return JAGG_OK;
@@ -449,11 +519,14 @@ extern "C" int jagg_gemm_fp8(const jagg_gemm_fp8_desc* d, cudaStream_t stream) {
     JAGG_CHECK_ARG(d->B && fp8::aligned(d->B, 16) && d->ldb % 16 == 0 && d->ldb >= b_cols,
                    "%s: B needs a 16-byte aligned base and a row pitch that is a multiple of 16 and >= %lld (got %lld)", who,
                    (long long)b_cols, (long long)d->ldb);
-    JAGG_CHECK_ARG(d->a_scale && fp8::aligned(d->a_scale, 4) && d->lda_scale >= d->M,
-                   "%s: A's scales null, misaligned, or with a pitch below M=%lld", who, (long long)d->M);
+    JAGG_CHECK_ARG(d->a_scale && fp8::aligned(d->a_scale, 16) && d->lda_scale % 4 == 0 && d->lda_scale >= d->M,
+                   "%s: A's scales need a 16-byte aligned base and a pitch that is a multiple of 4 and >= M=%lld (got %lld)",
+                   who, (long long)d->M, (long long)d->lda_scale);
     const int64_t b_need = !d->b_block ? d->N : d->b_trans ? ng : kg;
-    JAGG_CHECK_ARG(d->b_scale && fp8::aligned(d->b_scale, 4) && d->ldb_scale >= b_need,
-                   "%s: B's scales null, misaligned, or with a pitch below %lld", who, (long long)b_need);
+    JAGG_CHECK_ARG(d->b_scale && fp8::aligned(d->b_scale, d->b_block ? 4 : 16) &&
+                       (d->b_block || d->ldb_scale % 4 == 0) && d->ldb_scale >= b_need,
+                   "%s: B's scales null, misaligned, or with a pitch that does not fit: >= %lld%s (got %lld)", who,
+                   (long long)b_need, d->b_block ? "" : " and a multiple of 4", (long long)d->ldb_scale);
   }
   GemmFp8Args g;
   g.M = d->M; g.N = d->N; g.K = d->K;

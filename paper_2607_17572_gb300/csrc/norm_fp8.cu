@@ -515,13 +515,15 @@ __global__ void __launch_bounds__(256) quantize_kernel(const QuantParams p) {
   }
 }
 
-int check_out(const char* who, const char* form, const jagg_fp8_out* o, int64_t cols, int64_t lds) {
+// `step`: what the pitch of the scales is a multiple of (1: blocks, which need no alignment either).
+int check_out(const char* who, const char* form, const jagg_fp8_out* o, int64_t cols, int64_t lds, int step) {
   JAGG_CHECK_ARG(o->scale, "%s: %s codes without scales", who, form);
   JAGG_CHECK_ARG(aligned(o->q, 16) && o->ldq % 16 == 0 && o->ldq >= cols,
                  "%s: %s codes need a 16-byte aligned base and a row pitch that is a multiple of 16 and >= %lld (got %lld)",
                  who, form, (long long)cols, (long long)o->ldq);
-  JAGG_CHECK_ARG(aligned(o->scale, 4) && o->lds >= lds, "%s: %s scales: pitch %lld below %lld", who, form,
-                 (long long)o->lds, (long long)lds);
+  JAGG_CHECK_ARG(aligned(o->scale, 4 * step) && o->lds % step == 0 && o->lds >= lds,
+                 "%s: %s scales need a %d-byte aligned base and a pitch that is a multiple of %d and >= %lld (got %lld)", who,
+                 form, 4 * step, step, (long long)lds, (long long)o->lds);
   return JAGG_OK;
 }
 
@@ -550,7 +552,7 @@ extern "C" int jagg_rms_norm_fp8(const void* x, int x_dtype, int64_t ldx, const 
                  "%s: a pointer is not aligned to its elements", who);
   JAGG_CHECK_ARG(eps >= 0.f, "%s: eps must not be negative", who);
   const jagg_fp8_out o{q, ldq, scale, lds};
-  JAGG_TRY(check_out(who, "row", &o, d, rows));
+  JAGG_TRY(check_out(who, "row", &o, d, rows, 4));
   const NormParams p{x, ldx, residual, ldh, weight, w_dtype == JAGG_DTYPE_F32, rows, (int)d, eps, h_out, q, ldq,
                      scale, lds, rstd};
   const bool vec = d % 8 == 0 && aligned(x, 16) && ldx * xs % 16 == 0 && aligned(weight, 16) &&
@@ -633,9 +635,9 @@ extern "C" int jagg_quantize_fp8(const void* x, int x_dtype, int64_t ldx, int64_
   if (by_block && by_block->q) p.block = *by_block;
   JAGG_CHECK_ARG(p.row.q || p.col.q || p.block.q || rows == 0 || cols == 0, "%s: no form asked for", who);
   if (rows == 0 || cols == 0) return JAGG_OK;
-  if (p.row.q) JAGG_TRY(check_out(who, "row", &p.row, cols, rows));
-  if (p.col.q) JAGG_TRY(check_out(who, "column", &p.col, cols, cols));
-  if (p.block.q) JAGG_TRY(check_out(who, "block", &p.block, cols, gc));
+  if (p.row.q) JAGG_TRY(check_out(who, "row", &p.row, cols, rows, 4));
+  if (p.col.q) JAGG_TRY(check_out(who, "column", &p.col, cols, cols, 4));
+  if (p.block.q) JAGG_TRY(check_out(who, "block", &p.block, cols, gc, 1));
   JAGG_CHECK_ARG(x && ldx >= cols, "%s: null input or row pitch below cols=%lld", who, (long long)cols);
   const int xs = size_of(x_dtype);
   JAGG_CHECK_ARG(aligned(x, xs) && aligned(row_mul, 4) && aligned(col_mul, size_of(col_mul_dtype)),

@@ -31,7 +31,7 @@ NORM = dict(x=FAKE, x_dtype=1, ldx=64, residual=FAKE, h_dtype=0, ldh=64, weight=
     (dict(x=None), -1, "null"), (dict(q=None), -1, "null"), (dict(scale=None), -1, "null"), (dict(x_dtype=2), -1, "dtype"),
     (dict(rows=-1), -1, "rows"), (dict(d=0), -1, "d=0"), (dict(d=40000, ldx=40000, ldh=40000, ldq=40000), -2, "32768"),
     (dict(ldx=63), -1, "pitch"), (dict(ldh=63), -1, "pitch"), (dict(ldq=72), -1, "pitch"), (dict(ldq=48), -1, "pitch"),
-    (dict(lds=3), -1, "scales"), (dict(q=FAKE + 8), -1, "aligned"), (dict(x=FAKE + 1), -1, "aligned"),
+    (dict(lds=3), -1, "scales"), (dict(lds=6), -1, "scales"), (dict(scale=FAKE + 4), -1, "scales"), (dict(q=FAKE + 8), -1, "aligned"), (dict(x=FAKE + 1), -1, "aligned"),
     (dict(residual=FAKE + 2), -1, "aligned"), (dict(eps=-1.0), -1, "eps"), (dict(eps=float("nan")), -1, "eps")])
 def test_norm_refusals(jg, change, code, word):
     a = dict(NORM, **change)
@@ -62,7 +62,8 @@ def test_norm_backward_workspace(jg):
     (dict(block=(FAKE, 64, None, 1)), "without scales"), (dict(block=(FAKE + 4, 64, FAKE, 1)), "block"),
     (dict(block=(FAKE, 64, FAKE, 0)), "block"), (dict(row=(FAKE, 64, FAKE, 4), ldx=63), "pitch"),
     (dict(row=(FAKE, 64, FAKE, 4), x=None), "null"), (dict(row=(FAKE, 64, FAKE, 4), rows=1 << 24), "rows"),
-    (dict(row=(FAKE, 64, FAKE, 4), x_dtype=5), "dtype"), (dict(row=(FAKE, 64, FAKE, 4), row_mul=FAKE + 2), "aligned")])
+    (dict(row=(FAKE, 64, FAKE, 4), x_dtype=5), "dtype"), (dict(col=(FAKE, 64, FAKE + 8, 64)), "column"),
+    (dict(col=(FAKE, 64, FAKE, 66)), "column"), (dict(row=(FAKE, 64, FAKE, 4), row_mul=FAKE + 2), "aligned")])
 def test_quantise_refusals(jg, change, word):
     o = {f: ctypes.byref(jg.Fp8Out(*change[f])) if f in change else None for f in ("row", "col", "block")}
     st = jg.lib().jagg_quantize_fp8(change.get("x", FAKE), change.get("x_dtype", 1), change.get("ldx", 64),
@@ -79,7 +80,8 @@ GEMM = dict(M=8, N=200, K=300, A=FAKE, lda=304, a_scale=FAKE, lda_scale=8, B=FAK
     (dict(M=-1), "outside"), (dict(N=1 << 31), "outside"), (dict(A=None), "A needs"), (dict(lda=300), "A needs"),
     (dict(lda=288), "A needs"), (dict(A=FAKE + 8), "A needs"), (dict(ldb=300), "B needs"), (dict(B=None), "B needs"),
     (dict(a_scale=None), "A's scales"), (dict(lda_scale=7), "A's scales"), (dict(ldb_scale=2), "B's scales"),
-    (dict(b_block=0, ldb_scale=199), "B's scales"), (dict(b_trans=1, ldb=208, ldb_scale=1), "B's scales"),
+    (dict(b_block=0, ldb_scale=199), "B's scales"), (dict(b_block=0, ldb_scale=202), "B's scales"),
+    (dict(b_block=0, ldb_scale=200, b_scale=FAKE + 4), "B's scales"), (dict(lda_scale=10), "A's scales"), (dict(b_trans=1, ldb=208, ldb_scale=1), "B's scales"),
     (dict(a_trans=1, lda=0), "A needs"), (dict(C=None), "output"), (dict(ldc=199), "output"), (dict(C=FAKE + 1), "output"),
     (dict(accumulate=1), "accumulation"), (dict(c_dtype=3), "dtype"), (dict(bias=FAKE + 2), "bias")])
 def test_product_refusals(jg, change, word):

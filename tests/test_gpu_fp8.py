@@ -31,7 +31,7 @@ def _codes(rows, cols, form, pad=0):
     ld = -(-cols // 16) * 16 + pad
     raw = torch.full((rows + 2, ld), 0x55, dtype=torch.uint8, device="cuda")
     shape = {"row": (groups(cols), rows), "col": (groups(rows), cols), "block": (groups(rows), groups(cols))}[form]
-    s_raw = torch.full((shape[0] + 1, shape[1] + 3), -7.0, device="cuda")
+    s_raw = torch.full((shape[0] + 1, -(-shape[1] // 4) * 4 + 4), -7.0, device="cuda")
     return raw, raw[:rows, :cols], s_raw, s_raw[:shape[0], :shape[1]]
 
 
@@ -483,6 +483,8 @@ def test_refusals():
         jg.rms_norm_fp8(x.cpu(), q, s)
     with pytest.raises(jg.JaggError, match="pitch"):
         jg.rms_norm_fp8(x, torch.empty(4, 66, dtype=torch.float8_e4m3fn, device="cuda")[:, :64], s)
+    with pytest.raises(jg.JaggError, match="multiple of 4"):
+        jg.rms_norm_fp8(_rand(4, 200), jg.fp8_buffers(4, 200, "row")[0], torch.empty(2, 5, device="cuda")[:, :4])
     with pytest.raises(jg.JaggError, match="workspace"):
         jg.rms_norm_bwd(x, x, torch.empty(4, device="cuda"), torch.empty_like(x), dweight=torch.empty(64, device="cuda"))
     b, sb = jg.fp8_buffers(8, 64, "block")
