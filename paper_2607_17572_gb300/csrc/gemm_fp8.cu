@@ -14,11 +14,12 @@
 // CTAs splits K: each sums its k-blocks, the partial tiles meet in shared memory and every CTA
 // joins and stores its part of the tile, in the order of the ranks (no atomics, no workspace).
 //
-// Vector scales arrive by TMA beside the operands, in a ring of slots that outlives the operand
-// stages by the accumulators in flight; block scales are read 32 k-blocks at a time, one per lane.
+// Vector scales arrive by TMA beside the operands, eight k-blocks at a time; block scales are read 32
+// k-blocks at a time, one per lane.
 //
-// Roles: warp 0 TMA producer, warp 1 MMA issuer, warps 4 and up the epilogue (tensor-memory lanes
-// 32 (warp % 4) .. + 31, 64 or fewer columns); all warps join and store.
+// Roles: warp 0 TMA producer, warp 1 MMA issuer, warp 2 watches the accumulators' barriers for the
+// epilogue warps (which would slow each other down by polling), warps 4 and up the epilogue
+// (tensor-memory lanes 32 (warp % 4) .. + 31, 64 or fewer columns); all warps join and store.
 #include <atomic>
 #include <cmath>
 
@@ -31,6 +32,7 @@ int unit_status_gemm_fp8(unsigned* v, int clear) { return read_unit_status(v, cl
 namespace {
 
 using fp8::GROUP;
+using fp8::SCALE_KB;
 
 constexpr int F_ROWS = 128;                  // P rows of a tile
 constexpr int F_TILE = F_ROWS * GROUP;       // bytes of a whole operand tile of a k-block
@@ -51,9 +53,6 @@ struct FCfg {
   static constexpr int CW = NT < 64 ? NT : NT / 2;                  // columns of an epilogue warp
   static constexpr int EW = 4 * (NT / CW);                          // epilogue warps
   static constexpr int THREADS = 128 + 32 * EW;
-  // A slot is written for k-block i once the products of i - STAGES are done; those were issued
-  // after the epilogue had finished with k-block i - STAGES - F_ACCS.
-  static constexpr int SLOTS = STAGES + F_ACCS;
 };
 
 struct FParams {
@@ -81,10 +80,10 @@ __global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
   extern __shared__ uint8_t smem_f8[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_f8) + 1023) & ~uintptr_t(1023));
   __shared__ uint64_t full[F_MAX_STAGES], empty[F_MAX_STAGES], tfull[F_ACCS], tempty[F_ACCS], drainbar;
-  __shared__ uint64_t sfull[Cfg::SLOTS];
+  __shared__ uint64_t sfull[2], sempty[2];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int abort_flag;
-  __shared__ __align__(128) float pscale[Cfg::SLOTS][F_ROWS], qscale[Cfg::SLOTS][NT < 32 ? 32 : NT];
+  __shared__ __align__(128) float pscale[2][SCALE_KB][F_ROWS], qscale[2][SCALE_KB][NT];
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = p.splits > 1 ? (int)ptx::cluster_ctarank() : 0;
@@ -103,7 +102,10 @@ __global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
       ptx::mbar_init(&tfull[a], 1);
       ptx::mbar_init(&tempty[a], Cfg::EW);
     }
-    for (int i = 0; i < Cfg::SLOTS; ++i) ptx::mbar_init(&sfull[i], 1);
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(&sfull[i], 1);
+      ptx::mbar_init(&sempty[i], Cfg::EW);
+    }
     ptx::mbar_init(&drainbar, 1);
     ptx::fence_mbar_init();
     if (p.k_blocks > 0) {
@@ -130,9 +132,9 @@ __global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
   if (warp == 0) {
     if (ptx::elect_one()) {
       // ---------------- TMA producer
-      int stage = 0, slot = 0;
+      int stage = 0;
       uint32_t phase = 0, issued = 0, issued_parity = 0;
-      uint32_t s_phase = 0, s_issued = 0, s_parity = 0;
+      uint32_t slots = 0;  // of scales asked for so far
       for (int kb = kb0; kb < kb1; ++kb) {
         if (!ptx::mbar_wait(&empty[stage], phase ^ 1)) { abort_flag = 1; break; }
         uint8_t* sP = smem + stage * Cfg::STAGE;
@@ -145,12 +147,14 @@ __global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
           ptx::tma_load_2d(sP + F_TILE, &maps.q, &full[stage], q0, kb * GROUP);
         else
           ptx::tma_load_2d(sP + F_TILE, &maps.q, &full[stage], kb * GROUP, q0);
-        ptx::mbar_arrive_expect_tx(&sfull[slot], (p.p_block ? 0 : F_ROWS * 4) + (QVEC ? NT * 4 : 0));
-        if (!p.p_block) ptx::tma_load_2d(pscale[slot], &maps.ps, &sfull[slot], p0, kb);
-        if (QVEC) ptx::tma_load_2d(qscale[slot], &maps.qs, &sfull[slot], q0, kb);
-        s_issued |= 1u << slot;
-        s_parity = (s_parity & ~(1u << slot)) | (s_phase << slot);
-        if (++slot == Cfg::SLOTS) { slot = 0; s_phase ^= 1; }
+        if ((kb - kb0) % SCALE_KB == 0) {
+          const uint32_t slot = slots & 1;
+          if (!ptx::mbar_wait(&sempty[slot], ((slots >> 1) & 1) ^ 1)) { abort_flag = 1; break; }
+          ptx::mbar_arrive_expect_tx(&sfull[slot], SCALE_KB * 4 * ((p.p_block ? 0 : F_ROWS) + (QVEC ? NT : 0)));
+          if (!p.p_block) ptx::tma_load_2d(pscale[slot], &maps.ps, &sfull[slot], p0, kb);
+          if (QVEC) ptx::tma_load_2d(qscale[slot], &maps.qs, &sfull[slot], q0, kb);
+          ++slots;
+        }
         issued |= 1u << stage;
         issued_parity = (issued_parity & ~(1u << stage)) | (phase << stage);
         if (++stage == Cfg::STAGES) { stage = 0; phase ^= 1; }
@@ -158,8 +162,7 @@ __global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
       if (abort_flag) {  // after a give-up: loads already issued land before shared memory goes away
         for (int s = 0; s < Cfg::STAGES; ++s)
           if (issued & (1u << s)) ptx::mbar_wait(&full[s], (issued_parity >> s) & 1u);
-        for (int s = 0; s < Cfg::SLOTS; ++s)
-          if (s_issued & (1u << s)) ptx::mbar_wait(&sfull[s], (s_parity >> s) & 1u);
+        for (uint32_t n = slots > 2 ? slots - 2 : 0; n < slots; ++n) ptx::mbar_wait(&sfull[n & 1], (n >> 1) & 1);
       }
     }
   } else if (warp == 1) {
@@ -192,38 +195,59 @@ __global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
         ptx::mbar_wait(&drainbar, 0);
       }
     }
+  } else if (warp == 2) {
+    // ---------------- watcher
+    int a = 0;
+    uint32_t a_phase = 0;
+    bool alive = true;  // after a give-up the epilogue is let go without data, so that it ends
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (alive) alive = ptx::mbar_wait(&tfull[a], a_phase);
+      if (!alive) abort_flag = 1;
+      __syncwarp();
+#pragma unroll
+      for (int sl = 0; sl < Cfg::EW / 4; ++sl) fp8::named_arrive(1 + a * (Cfg::EW / 4) + sl, 160);
+      if (++a == F_ACCS) { a = 0; a_phase ^= 1; }
+    }
   } else if (warp >= 4) {
     // ---------------- epilogue: thread = P row, CW columns of Q
-    const int q4 = warp & 3, c0 = ((warp - 4) >> 2) * CW;
-    const int row = q4 * 32 + lane;
+    const int q4 = warp & 3, sl = (warp - 4) >> 2, c0 = sl * CW;
     const uint32_t t0 = tmem + ((uint32_t)(q4 * 32) << 16) + c0;
     // block scales of 32 k-blocks, one per lane, and of the 32 after them
     const bool block = p.p_block || !QVEC;
     const float* bs = p.block + (int64_t)((p.p_block ? p0 : q0) / GROUP) * p.block_step;
     auto block_at = [&](int kb) { return block && kb < kb1 ? bs[(int64_t)kb * p.block_ld] : 1.f; };
     float bcur = block_at(kb0 + lane), bnext = block_at(kb0 + 32 + lane);
-    int a = 0, slot = 0;
-    uint32_t a_phase = 0, s_phase = 0;
+    int a = 0;
+    uint32_t slots = 0, ps = 0, qs = 0;  // addresses of this k-block's scales: of the row, of the columns
+    bool alive = true;
     for (int kb = kb0; kb < kb1; ++kb) {
       const int at = (kb - kb0) & 31;
       if (at == 0 && kb > kb0) {
         bcur = bnext;
         bnext = block_at(kb + 32 + lane);
       }
+      if (at % SCALE_KB == 0) {
+        if (alive) alive = ptx::mbar_wait(&sfull[slots & 1], (slots >> 1) & 1);
+        ps = ptx::smem_u32(&pscale[slots & 1][0][q4 * 32 + lane]);
+        qs = ptx::smem_u32(&qscale[slots & 1][0][c0]);
+      }
       float s = __shfl_sync(0xffffffffu, bcur, at);
-      bool ok = !abort_flag && ptx::mbar_wait(&sfull[slot], s_phase);
-      if (!p.p_block) s *= pscale[slot][row];
-      ok = ok && ptx::mbar_wait(&tfull[a], a_phase);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) { abort_flag = 1; break; }
+      if (!p.p_block) s *= ptx::ld_shared(ps);
+      fp8::named_sync(1 + a * (Cfg::EW / 4) + sl, 160);  // the watcher has seen the accumulator complete
       ptx::tc_fence_after();
-      fp8::scaled_add<CW, QVEC, (CW < 32 ? 16 : 32)>(acc, t0 + a * NT, s, ptx::smem_u32(qscale[slot] + c0));
+      fp8::scaled_add<CW, QVEC, (CW < 32 ? 16 : 32)>(acc, t0 + a * NT, s, qs);
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&tempty[a]);
-      if (++a == F_ACCS) { a = 0; a_phase ^= 1; }
-      if (++slot == Cfg::SLOTS) { slot = 0; s_phase ^= 1; }
+      if (++a == F_ACCS) a = 0;
+      ps += F_ROWS * 4;
+      qs += NT * 4;
+      if (at % SCALE_KB == SCALE_KB - 1) {
+        if (lane == 0) ptx::mbar_arrive(&sempty[slots & 1]);
+        ++slots;
+      }
     }
+    if (!alive) abort_flag = 1;
   }
   ptx::tc_fence_before();
   __syncthreads();
@@ -349,8 +373,8 @@ int launch_f8(const GemmFp8Args& g, int splits, cudaStream_t s) {
   if (g.K > 0) {
     JAGG_TRY(fp8_operand_map(&maps.p, po, p.P, g.K, F_ROWS));
     JAGG_TRY(fp8_operand_map(&maps.q, qo, p.Q, g.K, NT));
-    if (!po.block) JAGG_TRY(fp8_scale_map(&maps.ps, po, p.P, g.K, F_ROWS, 1));
-    if (QVEC) JAGG_TRY(fp8_scale_map(&maps.qs, qo, p.Q, g.K, NT, 1));
+    if (!po.block) JAGG_TRY(fp8_scale_map(&maps.ps, po, p.P, g.K, F_ROWS, SCALE_KB));
+    if (QVEC) JAGG_TRY(fp8_scale_map(&maps.qs, qo, p.Q, g.K, NT, SCALE_KB));
   }
   auto kernel = gemm_fp8_kernel<NT, Q_MN, SWAP, QVEC>;
   static OncePerDevice once;

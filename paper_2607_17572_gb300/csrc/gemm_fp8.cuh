@@ -43,6 +43,15 @@ int fp8_scale_map(CUtensorMap* m, const Fp8Operand& o, int64_t rows, int64_t K, 
 
 namespace fp8 {
 
+constexpr int SCALE_KB = 8;  // k-blocks whose vector scales arrive in one load
+
+__device__ __forceinline__ void named_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+__device__ __forceinline__ void named_arrive(int id, int threads) {
+  asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
 // acc[j] += s d[j] (q[j]) over CW columns of an accumulator, from tensor-memory address `t`: the inner
 // sum of one group times its two scales.  s: the row's scale (times the columns' where they share one);
 // q: address of the columns' scales in shared memory when QVEC.

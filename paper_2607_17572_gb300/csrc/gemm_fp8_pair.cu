@@ -27,13 +27,13 @@ int unit_status_gemm_fp8_pair(unsigned* v, int clear) { return read_unit_status(
 namespace {
 
 using fp8::GROUP;
+using fp8::SCALE_KB;
 
 constexpr int W_ROWS = 256, W_MAX_N = 256;
 constexpr int W_ACCS = 2;             // accumulators in tensor memory
 constexpr int W_EW = 16, W_CW = 64;
 constexpr int W_THREADS = 128 + 32 * W_EW;
 constexpr int W_HALF = 128 * GROUP;   // bytes of a CTA's half of an operand tile
-constexpr int W_SCALE_KB = 8;         // k-blocks whose scales arrive in one load
 constexpr int W_MAX_STAGES = 6;
 constexpr int W_GROUP = 19;           // row tiles walked together (gemm_pair.cu)
 
@@ -43,7 +43,7 @@ struct WCfg {
   static constexpr int STEP = QVEC ? 8 : 16;
   static constexpr int BOX = QVEC ? 2048 : 1024;  // an epilogue warp's staging box: 32 rows of 64 or 32 bytes
   static constexpr int ROW = BOX / 32;
-  static constexpr int SLOT = W_SCALE_KB * (128 + (QVEC ? W_MAX_N : 0));  // floats: [kb][rows of A], [kb][columns of B]
+  static constexpr int SLOT = SCALE_KB * (128 + (QVEC ? W_MAX_N : 0));  // floats: [kb][rows of A], [kb][columns of B]
   static constexpr int SMEM = STAGES * 2 * W_HALF + W_EW * BOX + 2 * SLOT * 4 + 1024;
 };
 static_assert(WCfg<false>::SMEM <= 232448 - 1024 && WCfg<true>::SMEM <= 232448 - 1024, "shared memory");
@@ -69,13 +69,6 @@ __device__ __forceinline__ void w_decode(const WParams& p, int t, int& tm, int& 
   const int gm = min(W_GROUP, p.tiles_m - grp * W_GROUP);
   tm = grp * W_GROUP + in % gm;
   tn = in / gm;
-}
-
-__device__ __forceinline__ void named_sync(int id, int threads) {
-  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
-}
-__device__ __forceinline__ void named_arrive(int id, int threads) {
-  asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
 template <bool QVEC>
@@ -162,13 +155,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
             ptx::tma_load_2d_pair(sA + W_HALF, &maps.b, bar, nb, kb * GROUP);
           else
             ptx::tma_load_2d_pair(sA + W_HALF, &maps.b, bar, kb * GROUP, nb);
-          if (kb % W_SCALE_KB == 0) {
+          if (kb % SCALE_KB == 0) {
             const uint32_t slot = slots & 1;
             if (!ptx::mbar_wait(&sempty[slot], ((slots >> 1) & 1) ^ 1)) { abort_flag = 1; break; }
             float* sc = scales + slot * Cfg::SLOT;
             ptx::mbar_arrive_expect_tx(&sfull[slot], Cfg::SLOT * 4);
             ptx::tma_load_2d(sc, &maps.as, &sfull[slot], ma, kb);
-            if (QVEC) ptx::tma_load_2d(sc + W_SCALE_KB * 128, &maps.bs, &sfull[slot], tn * p.bn, kb);
+            if (QVEC) ptx::tma_load_2d(sc + SCALE_KB * 128, &maps.bs, &sfull[slot], tn * p.bn, kb);
             ++slots;
           }
           issued |= 1u << stage;
@@ -235,7 +228,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
         if (!alive) abort_flag = 1;
         __syncwarp();
 #pragma unroll
-        for (int sl = 0; sl < W_MAX_N / W_CW; ++sl) named_arrive(1 + a * (W_MAX_N / W_CW) + sl, 160);
+        for (int sl = 0; sl < W_MAX_N / W_CW; ++sl) fp8::named_arrive(1 + a * (W_MAX_N / W_CW) + sl, 160);
         if (++a == W_ACCS) { a = 0; a_phase ^= 1; }
       }
       if (!__all_sync(0xffffffffu, alive)) break;
@@ -266,18 +259,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
       uint32_t sc = 0, qc = 0;  // addresses of this k-block's scales: of the row, of the columns
 #pragma unroll 1
       for (int kb = 0; kb < p.k_blocks; ++kb) {
-        if (kb % W_SCALE_KB == 0) {
+        if (kb % SCALE_KB == 0) {
           if (!QVEC && kb % 32 == 0) {
             bcur = bnext;
             bnext = kb + 32 < p.k_blocks ? block_at(t, kb + 32 + lane) : block_at(t + npairs, lane);
           }
           if (alive) alive = ptx::mbar_wait(&sfull[slots & 1], (slots >> 1) & 1);
           sc = sbase + (slots & 1) * Cfg::SLOT * 4;
-          qc = sc + W_SCALE_KB * 128 * 4 + c0 * 4 - row4;
+          qc = sc + SCALE_KB * 128 * 4 + c0 * 4 - row4;
         }
         float s = ptx::ld_shared(sc);
         if (!QVEC) s *= __shfl_sync(0xffffffffu, bcur, kb & 31);
-        named_sync(1 + a * (W_MAX_N / W_CW) + sl, 160);  // the watcher has seen the accumulator complete
+        fp8::named_sync(1 + a * (W_MAX_N / W_CW) + sl, 160);  // the watcher has seen the accumulator complete
         ptx::tc_fence_after();
         fp8::scaled_add<W_CW, QVEC, Cfg::STEP>(acc, t0 + a * W_MAX_N, s, qc);
         ptx::tc_fence_before();
@@ -286,7 +279,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
         a ^= 1;
         sc += 128 * 4;
         qc += W_MAX_N * 4;
-        if (kb % W_SCALE_KB == W_SCALE_KB - 1 || kb == p.k_blocks - 1) {
+        if (kb % SCALE_KB == SCALE_KB - 1 || kb == p.k_blocks - 1) {
           if (lane == 0) ptx::mbar_arrive(&sempty[slots & 1]);
           ++slots;
         }
@@ -395,9 +388,9 @@ int launch_w8(const GemmFp8Args& g, int bn, cudaStream_t s) {
   WMaps maps;
   JAGG_TRY(fp8_operand_map(&maps.a, g.a, g.M, g.K, 128));
   JAGG_TRY(fp8_operand_map(&maps.b, g.b, g.N, g.K, bn / 2));
-  JAGG_TRY(fp8_scale_map(&maps.as, g.a, g.M, g.K, 128, W_SCALE_KB));
+  JAGG_TRY(fp8_scale_map(&maps.as, g.a, g.M, g.K, 128, SCALE_KB));
   maps.c = maps.bs = maps.as;  // unused ones
-  if (QVEC) JAGG_TRY(fp8_scale_map(&maps.bs, g.b, g.N, g.K, W_MAX_N, W_SCALE_KB));
+  if (QVEC) JAGG_TRY(fp8_scale_map(&maps.bs, g.b, g.N, g.K, W_MAX_N, SCALE_KB));
   if (p.c_tma) {
     const uint64_t dims[2] = {(uint64_t)g.N, (uint64_t)g.M};
     const uint64_t strides[1] = {(uint64_t)g.ldc * fp8::size_of(g.c_dtype)};

@@ -17,6 +17,7 @@ constexpr int CLIP_TENSORS = 1000;  // of a launch: the list fits the 32764 byte
 constexpr int CLIP_FEW = 100;       // a shorter list for launches of few tensors (3 KB to pass instead of 28)
 constexpr int CLIP_THREADS = 256;
 constexpr int CLIP_CHUNK = 32 * CLIP_THREADS;  // elements of a CTA's step: 8 or 4 16-byte loads per thread
+constexpr int CLIP_KEEP = 80 << 20;  // bytes that the first pass leaves in the L2 (129 MB) for the second
 constexpr int CLIP_CTAS_PER_SM = 4;
 constexpr int CLIP_CTAS = 640;  // most CTAs of a launch (rows of partial sums)
 
@@ -100,6 +101,7 @@ __global__ void __launch_bounds__(CLIP_THREADS) square_sum_kernel(const __grid_c
   pdl_wait();
   double sum = 0.0;
   const int total = l.first[l.count];
+  const int keep = total - CLIP_KEEP / (CLIP_CHUNK * (int)sizeof(T));  // from here on chunks are to stay in the L2
   for (int c = blockIdx.x; c < total; c += gridDim.x) {
     const int t = tensor_of(l, c);
     const T* g = static_cast<const T*>(l.in[t]);
@@ -108,8 +110,10 @@ __global__ void __launch_bounds__(CLIP_THREADS) square_sum_kernel(const __grid_c
     if (left >= CLIP_CHUNK && (reinterpret_cast<uintptr_t>(g) & 15) == 0) {
       uint4 w[VECS];
 #pragma unroll
-      for (int i = 0; i < VECS; ++i)
-        w[i] = *reinterpret_cast<const uint4*>(g + at + (int64_t)(i * CLIP_THREADS + threadIdx.x) * VEC);
+      for (int i = 0; i < VECS; ++i) {
+        const uint4* from = reinterpret_cast<const uint4*>(g + at + (int64_t)(i * CLIP_THREADS + threadIdx.x) * VEC);
+        w[i] = c < keep ? __ldcs(from) : *from;
+      }
 #pragma unroll
       for (int i = 0; i < VECS; ++i) unpack<T>(w[i], reinterpret_cast<float(&)[VEC]>(v[i * VEC]));
     } else {
@@ -168,8 +172,9 @@ __global__ void __launch_bounds__(CLIP_THREADS)
     out2[0] = (float)norm;
     out2[1] = coef;
   }
+  // last chunks first: the L2 still holds what the first pass read last
   const int total = l.first[l.count];
-  for (int c = blockIdx.x; c < total; c += gridDim.x) {
+  for (int c = total - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
     const int t = tensor_of(l, c);
     const T* g = static_cast<const T*>(l.in[t]);
     T* o = static_cast<T*>(l.out[t]);
@@ -179,14 +184,14 @@ __global__ void __launch_bounds__(CLIP_THREADS)
       uint4 w[VECS];
 #pragma unroll
       for (int i = 0; i < VECS; ++i)
-        w[i] = *reinterpret_cast<const uint4*>(g + at + (int64_t)(i * CLIP_THREADS + threadIdx.x) * VEC);
+        w[i] = __ldcs(reinterpret_cast<const uint4*>(g + at + (int64_t)(i * CLIP_THREADS + threadIdx.x) * VEC));
 #pragma unroll
       for (int i = 0; i < VECS; ++i) {
         float v[VEC];
         unpack<T>(w[i], v);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) v[j] *= coef;
-        *reinterpret_cast<uint4*>(o + at + (int64_t)(i * CLIP_THREADS + threadIdx.x) * VEC) = pack<T>(v);
+        __stcs(reinterpret_cast<uint4*>(o + at + (int64_t)(i * CLIP_THREADS + threadIdx.x) * VEC), pack<T>(v));
       }
     } else {
 #pragma unroll
@@ -266,7 +271,7 @@ int run_lists(const ClipCall& c) {
     JAGG_LAUNCHED();
     return JAGG_OK;
   }
-  for (int i = 0; i < lists; ++i) {
+  for (int i = lists - 1; i >= 0; --i) {
     const int ctas = ctas_of(all[i].first[all[i].count]);
     JAGG_CUDA_TRY(launch(clip_kernel<T, N>, ctas, CLIP_THREADS, 0, c.stream, all[i], (const double*)c.part, parts,
                          c.max_norm, c.eps, i == 0 ? 1 : 0, c.norm_out));

@@ -200,14 +200,59 @@ struct NormBwdParams {
   float* part;  // [gridDim.x][d] sums of dy xhat, or null
 };
 
-// Rows in strides over the grid; a thread's columns stay the same, so their weight and their sums
-// over rows live in registers.  One warp per row (blockDim.y rows at a time), or the whole CTA.
+// Eight consecutive elements as they lie in memory, on their way through registers.
+template <typename T>
+struct Raw8 {
+  uint4 w[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    const uint32_t u[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[sizeof(T) / 2 - 1].x, w[sizeof(T) / 2 - 1].y,
+                           w[sizeof(T) / 2 - 1].z, w[sizeof(T) / 2 - 1].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 2) {
+        v[2 * i] = __uint_as_float(u[i] << 16);
+        v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+      } else {
+        v[2 * i] = __uint_as_float(u[2 * i]);
+        v[2 * i + 1] = __uint_as_float(u[2 * i + 1]);
+      }
+    }
+  }
+};
 template <typename Y, typename H, int C>
-__global__ void __launch_bounds__(512) rms_norm_bwd_kernel(const NormBwdParams p) {
-  __shared__ float part[2][16];
-  extern __shared__ float cols[];  // [blockDim.y][d] when a CTA takes several rows
+struct BwdRow {  // a thread's part of one row: dy, h and dh of C runs of eight columns
+  Raw8<Y> y[C];
+  Raw8<H> h[C], g[C];
+  float rstd;
+  __device__ __forceinline__ void load(const NormBwdParams& p, int64_t row) {
+    rstd = p.rstd[row];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+      if (col < p.d) {
+        y[c].load(static_cast<const Y*>(p.dy) + row * p.lddy + col);
+        h[c].load(static_cast<const H*>(p.h) + row * p.ldh + col);
+        if (p.dh) g[c].load(static_cast<const H*>(p.dh) + row * p.ldg + col);
+      }
+    }
+  }
+};
+
+// A CTA holds blockDim.y row slots of blockDim.x threads (whole warps, C runs of eight columns per
+// thread) and walks the rows in strides; a thread's columns stay the same, so their weight and their
+// sums over rows live in registers.  The next row of a slot is on its way while the last one is
+// reduced and written.
+template <typename Y, typename H, int C>
+__global__ void __launch_bounds__(C == 1 ? 640 : 512, 1) rms_norm_bwd_kernel(const NormBwdParams p) {
+  __shared__ float part[2][20];
+  extern __shared__ float cols[];  // [blockDim.y][d] when a CTA has several slots
   pdl_wait();
-  const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, slot = threadIdx.y;
+  const float per_d = 1.f / (float)p.d;
   float w[C][8], dw[C][8];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
@@ -216,52 +261,58 @@ __global__ void __launch_bounds__(512) rms_norm_bwd_kernel(const NormBwdParams p
     for (int i = 0; i < 8; ++i) w[c][i] = 1.f, dw[c][i] = 0.f;
     if (p.weight && col < p.d) load8_any(p.weight, p.w_f32, col, w[c]);
   }
+  const int64_t step = (int64_t)gridDim.x * blockDim.y;
+  int64_t row = (int64_t)blockIdx.x * blockDim.y + slot;
+  BwdRow<Y, H, C> next;
+  if (row < p.rows) next.load(p, row);
   int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; row < p.rows;
-       row += (int64_t)gridDim.x * blockDim.y) {
-    const float rstd = p.rstd[row];
-    float g[C][8], xh[C][8], o[C][8];
+  for (; row < p.rows; row += step) {
+    const BwdRow<Y, H, C> r = next;
+    if (row + step < p.rows) next.load(p, row + step);
+    float g[C][8], xh[C][8], sum = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+      if ((c * (int)blockDim.x + (int)threadIdx.x) * 8 < p.d) {
+        r.y[c].values(g[c]);
+        r.h[c].values(xh[c]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[c][i] = xh[c][i] = o[c][i] = 0.f;
-      if (col < p.d) {
-        load8(static_cast<const Y*>(p.dy) + row * p.lddy + col, g[c]);
-        load8(static_cast<const H*>(p.h) + row * p.ldh + col, xh[c]);
-        if (p.dh) load8(static_cast<const H*>(p.dh) + row * p.ldg + col, o[c]);
+        for (int i = 0; i < 8; ++i) {
+          xh[c][i] *= r.rstd;
+          dw[c][i] = fmaf(g[c][i], xh[c][i], dw[c][i]);
+          g[c][i] *= w[c][i];
+          sum = fmaf(g[c][i], xh[c][i], sum);
+        }
       }
     }
-    float sum = 0.f;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        xh[c][i] *= rstd;
-        dw[c][i] = fmaf(g[c][i], xh[c][i], dw[c][i]);
-        g[c][i] *= w[c][i];
-        sum = fmaf(g[c][i], xh[c][i], sum);
-      }
     sum = warp_sum(sum);
-    if (warps > 1) {  // blockDim.y is 1: the whole CTA is at the same row
-      if (lane == 0) part[turn][warp] = sum;
-      __syncthreads();
-      sum = 0.f;
-      for (int k = 0; k < warps; ++k) sum += part[turn][k];
+    if (warps > 1) {  // the slot's warps meet; a slot's barrier is its own
+      float* at = &part[turn][slot * warps];
+      if (lane == 0) at[warp] = sum;
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + slot), "r"((int)blockDim.x) : "memory");
+      sum = warp_sum(lane < warps ? at[lane] : 0.f);
       turn ^= 1;
     }
-    const float mean = sum / (float)p.d;
+    const float mean = sum * per_d;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
+      if (col < p.d) {
+        float o[8];
+        if (p.dh) {
+          r.g[c].values(o);
+        } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[c][i] = fmaf(rstd, g[c][i] - xh[c][i] * mean, o[c][i]);
-      if (col < p.d) store8(static_cast<H*>(p.dx) + row * p.ldg + col, o[c]);
+          for (int i = 0; i < 8; ++i) o[i] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = fmaf(r.rstd, fmaf(-mean, xh[c][i], g[c][i]), o[i]);
+        store8(static_cast<H*>(p.dx) + row * p.ldg + col, o);
+      }
     }
   }
   if (!p.part) return;
   float* out = p.part + (int64_t)blockIdx.x * p.d;
-  if (blockDim.y > 1) out = cols + (int64_t)threadIdx.y * p.d;
+  if (blockDim.y > 1) out = cols + (int64_t)slot * p.d;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int col = (c * (int)blockDim.x + (int)threadIdx.x) * 8;
@@ -336,35 +387,54 @@ __global__ void __launch_bounds__(256) dweight_kernel(const float* part, int n, 
   }
 }
 
-constexpr int64_t BWD_VEC_MAX_D = 8192;  // 16 warps of two runs per thread
-constexpr int BWD_MAX_CTAS = 608;  // rows of partial sums in the workspace at most (four per SM)
-
-// CTAs of the backward pass: rows of the workspace.
-int bwd_ctas(int64_t rows, int64_t rows_per_cta) {
-  const int64_t n = (rows + rows_per_cta - 1) / rows_per_cta;
-  return (int)(n < BWD_MAX_CTAS ? n : BWD_MAX_CTAS);
+// Row slots of `warps` warps each: CTAs of about 16 warps, one per SM, as many CTAs as there are rows
+// where rows are few.
+constexpr int WALK_WARPS = 20;  // of a row, with 102 registers per thread
+struct Slots {
+  int slots, ctas;
+};
+Slots row_slots(int64_t rows, int warps) {
+  const int most = warps >= 16 ? 1 : 16 / warps < 15 ? 16 / warps : 15;  // a named barrier each
+  const int sms = sm_count();
+  const int64_t each = (rows + sms - 1) / sms;
+  Slots s;
+  s.slots = (int)(each < most ? each : most);
+  const int64_t ctas = (rows + s.slots - 1) / s.slots;
+  s.ctas = (int)(ctas < sms ? ctas : sms);
+  return s;
 }
+
+constexpr int64_t BWD_VEC_MAX_D = 8192;  // 16 warps of two runs per thread
+constexpr int BWD_MAX_CTAS = 608;        // rows of partial sums in the workspace at most (four CTAs per SM)
 
 template <typename Y, typename H>
 int launch_norm_bwd(const NormBwdParams& p, bool vec, float* dweight, int accumulate, cudaStream_t s) {
   int ctas;
   if (!vec) {
-    ctas = bwd_ctas(p.rows, 1);
+    ctas = (int)(p.rows < BWD_MAX_CTAS ? p.rows : BWD_MAX_CTAS);
     auto kernel = rms_norm_bwd_any_kernel<Y, H>;
     static OncePerDevice once;
     JAGG_CUDA_TRY(allow_smem(once, kernel, (int)NORM_MAX_D * 4));
     JAGG_CUDA_TRY(launch(kernel, ctas, 256, p.part ? (size_t)p.d * 4 : 0, s, p));
   } else {
     const int chunks = ceil_div(p.d, 256);
-    const int warps = ceil_div(chunks, 2), per = ceil_div(chunks, warps);
-    const int rows = warps == 1 ? 8 : 1;
-    ctas = bwd_ctas(p.rows, rows);
-    const dim3 block(32 * warps, rows);
-    const size_t smem = rows > 1 && p.part ? (size_t)rows * p.d * 4 : 0;
-    if (per == 1)
-      JAGG_CUDA_TRY(launch(rms_norm_bwd_kernel<Y, H, 1>, ctas, block, smem, s, p));
-    else
+    // A run per thread up to 20 warps, else two.  Two also for many bf16 rows where that keeps 14 warps
+    // or more busy: half the warps meet for a row (18432 x 4096: 122 us -> 111, 5000 x 1536 19.5 -> 16.9; but
+    // 9217 x 5120, 10 warps, 71 -> 90, and 300 x 4096 5.9 -> 6.4).
+    const int half = ceil_div(chunks, 2);
+    const bool two = chunks > WALK_WARPS ||
+                     (sizeof(Y) + sizeof(H) == 4 && chunks % 2 == 0 && half <= 8 && 16 / half * half >= 14 &&
+                      p.rows >= 16 * (int64_t)sm_count());
+    const int per = two ? 2 : 1, warps = two ? half : chunks;
+    const Slots sl = row_slots(p.rows, warps);
+    const int slots = sl.slots;
+    ctas = sl.ctas < BWD_MAX_CTAS ? sl.ctas : BWD_MAX_CTAS;
+    const dim3 block(32 * warps, slots);
+    const size_t smem = slots > 1 && p.part ? (size_t)slots * p.d * 4 : 0;
+    if (per == 2)
       JAGG_CUDA_TRY(launch(rms_norm_bwd_kernel<Y, H, 2>, ctas, block, smem, s, p));
+    else
+      JAGG_CUDA_TRY(launch(rms_norm_bwd_kernel<Y, H, 1>, ctas, block, smem, s, p));
   }
   JAGG_LAUNCHED();
   if (p.part) {
@@ -386,52 +456,90 @@ struct QuantParams {
   jagg_fp8_out row, col, block;
 };
 
+// Eight elements of a tile held between the passes over it: as f32, or as they were read (half the
+// registers for bf16, so that twice as many CTAs are resident: 4608 x 4096 in bf16, row and column
+// groups, 25.2 -> 16.5 us).
+template <typename T>
+struct Kept8 {
+  float v[8];
+  __device__ __forceinline__ float at(int i) const { return v[i]; }
+  __device__ __forceinline__ void set(int i, float x) { v[i] = x; }
+  __device__ __forceinline__ void forget() {}
+};
+template <>
+struct Kept8<bf16> {
+  uint32_t w[4];
+  __device__ __forceinline__ float at(int i) const {
+    return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+  }
+  // The compiler forgets what it has unpacked (it would keep both forms in registers).
+  __device__ __forceinline__ void forget() {
+    asm volatile("" : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]));
+  }
+  __device__ __forceinline__ void set(int i, float x) {
+    const uint32_t b = __bfloat16_as_ushort(__float2bfloat16_rn(x));  // exact: x is a bf16 value
+    w[i >> 1] = i & 1 ? (w[i >> 1] & 0xffffu) | (b << 16) : (w[i >> 1] & 0xffff0000u) | b;
+  }
+};
+
 // A 128 x 128 tile per CTA of 256 threads: thread (c, r) = (t & 15, t >> 4) holds columns 8 c .. + 7 of
 // the rows r, r + 16, .., r + 112, so a row group is one half warp's and a column group is 16
-// threads' eight rows each, joined in shared memory.
-template <typename X, bool VEC>
-__global__ void __launch_bounds__(256) quantize_kernel(const QuantParams p) {
+// threads' eight rows each, joined in shared memory.  K: what a thread keeps its elements as (bf16
+// only where no multipliers change them).
+template <typename X, typename K, bool VEC>
+__global__ void __launch_bounds__(256, sizeof(K) == 2 ? (VEC ? 4 : 3) : 2) quantize_kernel(const QuantParams p) {
   __shared__ float peak[16][GROUP];
   __shared__ float whole[8];
   pdl_wait();
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
   const int64_t row0 = (int64_t)blockIdx.y * GROUP, col0 = (int64_t)blockIdx.x * GROUP + 8 * c;
   const int live = (int)(p.cols - col0 < 0 ? 0 : p.cols - col0 < 8 ? p.cols - col0 : 8);  // columns of this thread
-  float v[8][8];
+  Kept8<K> v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t row = row0 + r + 16 * i;
+    const X* x = static_cast<const X*>(p.x) + row * p.ldx + col0;
+    if constexpr (VEC && sizeof(X) == 2 && sizeof(K) == 2) {
+      uint4 w = make_uint4(0, 0, 0, 0);
+      if (row < p.rows && live) w = *reinterpret_cast<const uint4*>(x);
+      v[i].w[0] = w.x; v[i].w[1] = w.y; v[i].w[2] = w.z; v[i].w[3] = w.w;
+    } else {
+      float f[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-    if (row < p.rows) {
-      const X* x = static_cast<const X*>(p.x) + row * p.ldx + col0;
-      if (VEC) {
-        if (live) load8(x, v[i]);
-      } else {
+      for (int j = 0; j < 8; ++j) f[j] = 0.f;
+      if (row < p.rows) {
+        if (VEC) {
+          if (live) load8(x, f);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j < live) f[j] = ld(x + j);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i].set(j, f[j]);
+    }
+  }
+  if constexpr (sizeof(K) == 4) {
+    if (p.row_mul) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t row = row0 + r + 16 * i;
+        const float m = row < p.rows ? p.row_mul[row] : 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (j < live) v[i][j] = ld(x + j);
+          if (row < p.rows && j < live) v[i].v[j] *= m;
       }
     }
-  }
-  if (p.row_mul) {
+    if (p.col_mul) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t row = row0 + r + 16 * i;
-      const float m = row < p.rows ? p.row_mul[row] : 0.f;
+      for (int j = 0; j < 8; ++j) {
+        if (j >= live) continue;
+        const float m = load_any(p.col_mul, p.col_f32, col0 + j);
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (row < p.rows && j < live) v[i][j] *= m;
-    }
-  }
-  if (p.col_mul) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (j >= live) continue;
-      const float m = load_any(p.col_mul, p.col_f32, col0 + j);
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (row0 + r + 16 * i < p.rows) v[i][j] *= m;
+        for (int i = 0; i < 8; ++i)
+          if (row0 + r + 16 * i < p.rows) v[i].v[j] *= m;
+      }
     }
   }
   auto put = [&](uint8_t* q, int64_t ldq, int64_t row, const float (&o)[8], float inv) {
@@ -449,12 +557,16 @@ __global__ void __launch_bounds__(256) quantize_kernel(const QuantParams p) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t row = row0 + r + 16 * i;
-      float a = 0.f;
+      float o[8], a = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) a = amax(a, v[i][j]);
+      for (int j = 0; j < 8; ++j) {
+        o[j] = v[i].at(j);
+        a = amax(a, o[j]);
+      }
+      v[i].forget();
       const float s = scale_of(half_warp_amax(a));
       if (row < p.rows && live) {
-        put(p.row.q, p.row.ldq, row, v[i], 1.f / s);
+        put(p.row.q, p.row.ldq, row, o, 1.f / s);
         if (c == 0) p.row.scale[(int64_t)blockIdx.x * p.row.lds + row] = s;
       }
     }
@@ -464,9 +576,11 @@ __global__ void __launch_bounds__(256) quantize_kernel(const QuantParams p) {
     for (int j = 0; j < 8; ++j) {
       float a = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) a = amax(a, v[i][j]);
+      for (int i = 0; i < 8; ++i) a = amax(a, v[i].at(j));
       peak[r][8 * c + j] = a;
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i].forget();
     __syncthreads();
     if (threadIdx.x < GROUP) {
       float a = 0.f;
@@ -487,9 +601,10 @@ __global__ void __launch_bounds__(256) quantize_kernel(const QuantParams p) {
       if (row < p.rows && live) {
         float o[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = v[i][j] * inv[j];
+        for (int j = 0; j < 8; ++j) o[j] = v[i].at(j) * inv[j];
         put(p.col.q, p.col.ldq, row, o, 1.f);
       }
+      v[i].forget();
     }
   }
   if (p.block.q) {
@@ -497,7 +612,9 @@ __global__ void __launch_bounds__(256) quantize_kernel(const QuantParams p) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) a = amax(a, v[i][j]);
+      for (int j = 0; j < 8; ++j) a = amax(a, v[i].at(j));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i].forget();
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) a = amax(a, __shfl_xor_sync(0xffffffffu, a, o));
     if ((threadIdx.x & 31) == 0) whole[threadIdx.x >> 5] = a;
@@ -510,9 +627,24 @@ __global__ void __launch_bounds__(256) quantize_kernel(const QuantParams p) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t row = row0 + r + 16 * i;
-      if (row < p.rows && live) put(p.block.q, p.block.ldq, row, v[i], inv);
+      if (row < p.rows && live) {
+        float o[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = v[i].at(j);
+        put(p.block.q, p.block.ldq, row, o, inv);
+      }
     }
   }
+}
+
+template <typename X, typename K>
+int launch_quant(const QuantParams& p, bool vec, dim3 grid, cudaStream_t s) {
+  if (vec)
+    JAGG_CUDA_TRY(launch(quantize_kernel<X, K, true>, grid, 256, 0, s, p));
+  else
+    JAGG_CUDA_TRY(launch(quantize_kernel<X, K, false>, grid, 256, 0, s, p));
+  JAGG_LAUNCHED();
+  return JAGG_OK;
 }
 
 // `step`: what the pitch of the scales is a multiple of (1: blocks, which need no alignment either).
@@ -645,18 +777,12 @@ extern "C" int jagg_quantize_fp8(const void* x, int x_dtype, int64_t ldx, int64_
   const bool vec = cols % 8 == 0 && aligned(x, 16) && ldx * xs % 16 == 0;
   const dim3 grid((unsigned)gc, (unsigned)gr);
   const int tok = prof_start(stream);
-  if (x_dtype == JAGG_DTYPE_F32) {
-    if (vec)
-      JAGG_CUDA_TRY(launch(quantize_kernel<float, true>, grid, 256, 0, stream, p));
-    else
-      JAGG_CUDA_TRY(launch(quantize_kernel<float, false>, grid, 256, 0, stream, p));
-  } else {
-    if (vec)
-      JAGG_CUDA_TRY(launch(quantize_kernel<bf16, true>, grid, 256, 0, stream, p));
-    else
-      JAGG_CUDA_TRY(launch(quantize_kernel<bf16, false>, grid, 256, 0, stream, p));
-  }
-  JAGG_LAUNCHED();
+  if (x_dtype == JAGG_DTYPE_F32)
+    JAGG_TRY((launch_quant<float, float>(p, vec, grid, stream)));
+  else if (row_mul || col_mul)
+    JAGG_TRY((launch_quant<bf16, float>(p, vec, grid, stream)));
+  else
+    JAGG_TRY((launch_quant<bf16, bf16>(p, vec, grid, stream)));
   prof_stop(tok, stream, PROF_QUANT_FP8, 0.0,
             (double)rows * cols * (xs + (p.row.q != nullptr) + (p.col.q != nullptr) + (p.block.q != nullptr)));
   return JAGG_OK;
