@@ -11,6 +11,7 @@
 
 #include <stdint.h>
 #include <cuda_runtime_api.h>
+#include "jagg.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -147,6 +148,11 @@ int jagg_test_colsum(const void* X, int x_f32, int rows, int cols, int64_t ld, f
  * flight.  out device [2] u64: out[0] = 1 when the wait gave up, out[1] = the nanoseconds
  * it waited. */
 int jagg_test_wait_timeout(unsigned long long limit_ns, unsigned long long* out, cudaStream_t stream);
+
+/* jagg_gemm_fp8 by a given kernel: CTA pairs with tiles of `pair` (128 or 256) columns, or, with pair = 0,
+ * single CTAs with K split over clusters of `splits` (1 to 8, at most ceil(K / 128)) and an accumulator
+ * of nt = 128 columns of B, or with swap nt = 16, 32 or 64 rows of A (a_trans = 0 only). */
+int jagg_test_gemm_fp8(const jagg_gemm_fp8_desc* desc, int pair, int nt, int splits, int swap, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -138,6 +138,7 @@ _SIGNATURES = {
     "jagg_grad_clip_workspace_bytes": (_I64, [_I]),
     "jagg_grad_norm": (_I, [_P, _P, _I, _I, _P, _P, _SZ, _P]),
     "jagg_grad_clip": (_I, [_P, _P, _P, _I, _I, _D, _D, _P, _P, _SZ, _P]),
+    "jagg_test_gemm_fp8": (_I, [ctypes.POINTER(GemmFp8Desc), _I, _I, _I, _I, _P]),
     "jagg_test_gemm": (_I, [ctypes.POINTER(GemmDesc), _P]),
     "jagg_test_gemm_pair": (_I, [ctypes.POINTER(GemmDesc), ctypes.POINTER(GemmDesc), _I, _I, _I, _I, _P]),
     "jagg_test_wait_timeout": (_I, [ctypes.c_ulonglong, _P, _P]),
@@ -603,12 +604,7 @@ def quantize_fp8(x, row=None, col=None, block=None, row_mul=None, col_mul=None, 
             _out(block, dev, rows, cols, gr, gc, "block"))
 
 
-def gemm_fp8(a, a_scale, b, b_scale, c, a_trans: bool = False, b_trans: bool = False, bias=None,
-             accumulate: bool = False, stream=None):
-    """c [M, N] (+)= A B^T (+ bias) of 8-bit operands (jagg_gemm_fp8).  a is [M, K] with row groups,
-    or with a_trans [K, M] with column groups; b is [N, K] with row groups or blocks, or with
-    b_trans [K, N] with column groups or blocks: which, is seen from the shape of b_scale."""
-    dev = c.get_device()
+def _fp8_desc(a, a_scale, b, b_scale, c, a_trans, b_trans, bias, accumulate, dev):
     M, N = c.shape
     K = a.shape[0] if a_trans else a.shape[1]
     gk = _groups(K)
@@ -626,7 +622,17 @@ def gemm_fp8(a, a_scale, b, b_scale, c, a_trans: bool = False, b_trans: bool = F
                     a_trans, b_trans, block, cd, DTYPE_F32, accumulate)
     if bias is not None:
         d.bias, d.bias_dtype = _vec(bias, dev, N, "bias")
-    _launch(dev, stream, "jagg_gemm_fp8", d)
+    return d
+
+
+def gemm_fp8(a, a_scale, b, b_scale, c, a_trans: bool = False, b_trans: bool = False, bias=None,
+             accumulate: bool = False, stream=None):
+    """c [M, N] (+)= A B^T (+ bias) of 8-bit operands (jagg_gemm_fp8).  a is [M, K] with row groups,
+    or with a_trans [K, M] with column groups; b is [N, K] with row groups or blocks, or with
+    b_trans [K, N] with column groups or blocks: which, is seen from the shape of b_scale."""
+    dev = c.get_device()
+    _launch(dev, stream, "jagg_gemm_fp8",
+            _fp8_desc(a, a_scale, b, b_scale, c, a_trans, b_trans, bias, accumulate, dev))
 
 
 # ----------------------------------------------------------------------------- gradient norm and clipping
@@ -714,6 +720,14 @@ def device_status(clear: bool = True) -> int:
 # ----------------------------------------------------------------------------- kernel tests
 def test_gemm(desc: GemmDesc, stream=None):
     _check(lib().jagg_test_gemm(ctypes.byref(desc), _stream(stream)), "jagg_test_gemm")
+
+
+def test_gemm_fp8(a, a_scale, b, b_scale, c, a_trans=False, b_trans=False, bias=None, accumulate=False, pair=0, nt=128,
+                  splits=1, swap=False, stream=None):
+    """gemm_fp8 by a given kernel (jagg_test_gemm_fp8)."""
+    dev = c.get_device()
+    _launch(dev, stream, "jagg_test_gemm_fp8",
+            _fp8_desc(a, a_scale, b, b_scale, c, a_trans, b_trans, bias, accumulate, dev), pair, nt, splits, int(swap))
 
 
 def test_gemm_pair(x: GemmDesc, y=None, bn=(0, 0), splits=(1, 1), stream=None):

@@ -23,6 +23,7 @@
 #include <atomic>
 #include <cmath>
 
+#include "../../include/jagg_testing.h"
 #include "gemm_fp8.cuh"
 
 namespace jagg {
@@ -397,13 +398,6 @@ int launch_f8(const GemmFp8Args& g, int splits, cudaStream_t s) {
   return JAGG_OK;
 }
 
-// How a product is computed: by CTA pairs in tiles of `pair` columns (0: by single CTAs, whose tile has
-// `nt` rows of Q, K split over clusters of `splits`).
-struct Plan {
-  int pair, nt, splits;
-  bool swap;
-};
-
 // Microseconds that a k-block takes, by kernel and tile, and what a tile and a launch take besides;
 // measured on 4096 x 4096 weights with 128 to 8192 rows, and on weight gradients of that size.  B's
 // vector scales cost a multiplication per element more than block scales.
@@ -439,13 +433,13 @@ int cluster_ctas(int n, int* ctas) {
   return JAGG_OK;
 }
 
-int plan_of(const GemmFp8Args& g, Plan* plan) {
+int plan_of(const GemmFp8Args& g, Fp8Plan* plan) {
   const int kb = ceil_div(g.K, GROUP), sms = sm_count();
   int room[F_MAX_SPLITS + 1] = {0, sms};
   for (int s = 2; s <= F_MAX_SPLITS; ++s) JAGG_TRY(cluster_ctas(s, &room[s]));
-  Plan& best = *plan;
+  Fp8Plan& best = *plan;
   double least = 0.0;
-  auto offer = [&](const Plan& p, double us) {
+  auto offer = [&](const Fp8Plan& p, double us) {
     if (least == 0.0 || us < least) {
       least = us;
       best = p;
@@ -472,7 +466,7 @@ int plan_of(const GemmFp8Args& g, Plan* plan) {
   return JAGG_OK;
 }
 
-int run_plan(const GemmFp8Args& g, const Plan& p, cudaStream_t s) {
+int run_plan(const GemmFp8Args& g, const Fp8Plan& p, cudaStream_t s) {
   if (p.pair) return gemm_fp8_pair(g, p.pair, s);
   if (p.swap) {
     if (p.nt == 16) return launch_f8<16, false, true, true>(g, p.splits, s);
@@ -503,9 +497,13 @@ int fp8_scale_map(CUtensorMap* m, const Fp8Operand& o, int64_t rows, int64_t K, 
 }
 
 int gemm_fp8(const GemmFp8Args& g, cudaStream_t s) {
-  const int tok = prof_start(s);
-  Plan p;
+  Fp8Plan p;
   JAGG_TRY(plan_of(g, &p));
+  return gemm_fp8_as(g, p, s);
+}
+
+int gemm_fp8_as(const GemmFp8Args& g, const Fp8Plan& p, cudaStream_t s) {
+  const int tok = prof_start(s);
   JAGG_TRY(run_plan(g, p, s));
   prof_stop(tok, s, PROF_GEMM_FP8, 2.0 * g.M * g.N * g.K,
             (double)g.M * g.K + (double)g.N * g.K + (double)g.M * g.N * (g.c_dtype == JAGG_DTYPE_F32 ? 4 : 2), (int)g.M,
@@ -517,8 +515,9 @@ int gemm_fp8(const GemmFp8Args& g, cudaStream_t s) {
 
 using namespace jagg;
 
-extern "C" int jagg_gemm_fp8(const jagg_gemm_fp8_desc* d, cudaStream_t stream) {
-  const char* who = "jagg_gemm_fp8";
+// The product that a descriptor asks for; *empty: there is nothing to compute.
+static int fp8_args(const char* who, const jagg_gemm_fp8_desc* d, GemmFp8Args* args, bool* empty) {
+  *empty = false;
   JAGG_CHECK_ARG(d, "%s: null descriptor", who);
   JAGG_CHECK_ARG(d->M >= 0 && d->N >= 0 && d->K >= 0 && d->M < INT32_MAX - 256 && d->N < INT32_MAX - 256 &&
                      d->K < INT32_MAX - 256,
@@ -530,7 +529,8 @@ extern "C" int jagg_gemm_fp8(const jagg_gemm_fp8_desc* d, cudaStream_t stream) {
   }
   JAGG_CHECK_ARG(fp8::is_dtype(d->c_dtype) && fp8::is_dtype(d->bias_dtype), "%s: bad dtype", who);
   JAGG_CHECK_ARG(!d->accumulate || d->c_dtype == JAGG_DTYPE_F32, "%s: accumulation needs an f32 output", who);
-  if (d->M == 0 || d->N == 0) return JAGG_OK;
+  *empty = d->M == 0 || d->N == 0;
+  if (*empty) return JAGG_OK;
   JAGG_CHECK_ARG(d->C && d->ldc >= d->N && fp8::aligned(d->C, fp8::size_of(d->c_dtype)),
                  "%s: output null, misaligned, or with a row pitch below N=%lld", who, (long long)d->N);
   JAGG_CHECK_ARG(fp8::aligned(d->bias, fp8::size_of(d->bias_dtype)), "%s: bias is not aligned to its elements", who);
@@ -552,7 +552,7 @@ extern "C" int jagg_gemm_fp8(const jagg_gemm_fp8_desc* d, cudaStream_t stream) {
                    "%s: B's scales null, misaligned, or with a pitch that does not fit: >= %lld%s (got %lld)", who,
                    (long long)b_need, d->b_block ? "" : " and a multiple of 4", (long long)d->ldb_scale);
   }
-  GemmFp8Args g;
+  GemmFp8Args& g = *args;
   g.M = d->M; g.N = d->N; g.K = d->K;
   g.a.q = d->A; g.a.ldq = d->lda; g.a.scale = d->a_scale; g.a.ld = d->lda_scale; g.a.mn = d->a_trans != 0;
   g.b.q = d->B; g.b.ldq = d->ldb; g.b.scale = d->b_scale; g.b.mn = d->b_trans != 0; g.b.block = d->b_block != 0;
@@ -562,5 +562,29 @@ extern "C" int jagg_gemm_fp8(const jagg_gemm_fp8_desc* d, cudaStream_t stream) {
   g.C = d->C; g.ldc = d->ldc; g.c_dtype = d->c_dtype;
   g.bias = d->bias; g.bias_dtype = d->bias_dtype;
   g.accumulate = d->accumulate != 0;
-  return gemm_fp8(g, stream);
+  return JAGG_OK;
+}
+
+extern "C" int jagg_gemm_fp8(const jagg_gemm_fp8_desc* desc, cudaStream_t stream) {
+  GemmFp8Args g;
+  bool empty;
+  JAGG_TRY(fp8_args("jagg_gemm_fp8", desc, &g, &empty));
+  return empty ? JAGG_OK : gemm_fp8(g, stream);
+}
+
+extern "C" int jagg_test_gemm_fp8(const jagg_gemm_fp8_desc* desc, int pair, int nt, int splits, int swap,
+                                  cudaStream_t stream) {
+  const char* who = "jagg_test_gemm_fp8";
+  GemmFp8Args g;
+  bool empty;
+  JAGG_TRY(fp8_args(who, desc, &g, &empty));
+  const int kb = ceil_div(g.K, GROUP);
+  JAGG_CHECK_ARG(!empty && kb > 0, "%s: an empty product", who);
+  if (pair) {
+    JAGG_CHECK_ARG(pair == 128 || pair == 256, "%s: pair tiles of %d columns", who, pair);
+  } else {
+    JAGG_CHECK_ARG(splits >= 1 && splits <= F_MAX_SPLITS && splits <= kb, "%s: %d splits of %d k-blocks", who, splits, kb);
+    JAGG_CHECK_ARG(swap ? (nt == 16 || nt == 32 || nt == 64) && !g.a.mn : nt == 128, "%s: tiles of %d columns", who, nt);
+  }
+  return gemm_fp8_as(g, {pair, nt, splits, swap != 0}, stream);
 }

@@ -30,8 +30,15 @@ struct GemmFp8Args {
   bool accumulate = false;
 };
 
-// One CTA per tile, or a cluster that splits K (gemm_fp8.cu); CTA pairs (gemm_fp8_pair.cu).
+// How a product is computed: by CTA pairs in tiles of `pair` columns (gemm_fp8_pair.cu; 0: not), or by
+// one CTA per tile or a cluster of `splits` that splits K (gemm_fp8.cu), the accumulator's columns being
+// 128 of B, or with `swap` `nt` rows of A.
+struct Fp8Plan {
+  int pair, nt, splits;
+  bool swap;
+};
 int gemm_fp8(const GemmFp8Args& g, cudaStream_t s);
+int gemm_fp8_as(const GemmFp8Args& g, const Fp8Plan& p, cudaStream_t s);
 int gemm_fp8_pair(const GemmFp8Args& g, int bn, cudaStream_t s);
 
 // Tensor map of a K-major operand (boxes of `box_rows` rows x 128 codes) or an MN-major one (128 rows of K x

@@ -114,57 +114,97 @@ __global__ void __launch_bounds__(1024) rms_norm_fp8_kernel(const NormParams p) 
   }
 }
 
-// Any width and alignment: one CTA per row, element by element, the row read twice.
-template <typename X, typename H>
-__global__ void __launch_bounds__(256) rms_norm_fp8_any_kernel(const NormParams p) {
-  __shared__ float part[8];
+// Rows of any width and alignment, element by element: a CTA of eight warps per row, and in it a warp
+// takes whole groups of 128 columns (its lanes four columns each, 32 apart): group warp, warp + 8, ..
+// G of them are held in registers; a longer row is read again (from the L2) for the second pass.
+constexpr int ANY_WARPS = 8;
+template <typename X, typename H, int G>
+__global__ void __launch_bounds__(32 * ANY_WARPS) rms_norm_fp8_any_kernel(const NormParams p) {
+  __shared__ float part[ANY_WARPS];
   pdl_wait();
   const int64_t row = blockIdx.x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const X* x = static_cast<const X*>(p.x) + row * p.ldx;
   const H* r = p.residual ? static_cast<const H*>(p.residual) + row * p.ldh : nullptr;
   H* h = p.h_out ? static_cast<H*>(p.h_out) + row * p.ldh : nullptr;
-  float ss = 0.f;
-  for (int c = threadIdx.x; c < p.d; c += 256) {
-    const float v = kept<H>(ld(x + c) + (r ? ld(r + c) : 0.f));
-    if (h) st(h + c, v);
-    ss = fmaf(v, v, ss);
-  }
-  ss = warp_sum(ss);
-  if (lane == 0) part[warp] = ss;
-  __syncthreads();  // also: h is written before any thread reads it back
-  ss = 0.f;
-  for (int w = 0; w < 8; ++w) ss += part[w];
-  const float rstd = 1.f / sqrtf(ss / (float)p.d + p.eps);
-  if (p.rstd && threadIdx.x == 0) p.rstd[row] = rstd;
-  for (int g0 = warp * GROUP; g0 < p.d; g0 += 8 * GROUP) {
-    float v[4], a = 0.f;
+  auto column = [&](int g, int i) { return (warp + g * ANY_WARPS) * GROUP + lane + 32 * i; };
+  const int groups = (p.d + GROUP * ANY_WARPS - 1) / (GROUP * ANY_WARPS);  // of a warp
+  float v[G][4], ss = 0.f;
+#pragma unroll
+  for (int g = 0; g < G; ++g)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int c = g0 + lane + 32 * i;
-      v[i] = 0.f;
-      if (c < p.d) {
-        const float hv = h ? ld(h + c) : kept<H>(ld(x + c) + (r ? ld(r + c) : 0.f));
-        v[i] = hv * rstd * (p.weight ? load_any(p.weight, p.w_f32, c) : 1.f);
-      }
-      a = amax(a, v[i]);
+      const int c = column(g, i);
+      v[g][i] = c < p.d ? ld(x + c) + (r ? ld(r + c) : 0.f) : 0.f;
+    }
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = column(g, i);
+      v[g][i] = kept<H>(v[g][i]);
+      if (h && c < p.d) st(h + c, v[g][i]);
+      ss = fmaf(v[g][i], v[g][i], ss);
+    }
+  for (int g = G; g < groups; ++g)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = column(g, i);
+      if (c >= p.d) continue;
+      const float f = kept<H>(ld(x + c) + (r ? ld(r + c) : 0.f));
+      if (h) st(h + c, f);
+      ss = fmaf(f, f, ss);
+    }
+  ss = warp_sum(ss);
+  if (lane == 0) part[warp] = ss;
+  __syncthreads();
+  ss = 0.f;
+  for (int w = 0; w < ANY_WARPS; ++w) ss += part[w];
+  const float rstd = 1.f / sqrtf(ss / (float)p.d + p.eps);
+  if (p.rstd && threadIdx.x == 0) p.rstd[row] = rstd;
+  auto put = [&](int g, float (&f)[4]) {
+    float a = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = column(g, i);
+      f[i] = c < p.d ? f[i] * rstd * (p.weight ? load_any(p.weight, p.w_f32, c) : 1.f) : 0.f;
+      a = amax(a, f[i]);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) a = amax(a, __shfl_xor_sync(0xffffffffu, a, o));
     const float s = scale_of(a), inv = 1.f / s;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int c = g0 + lane + 32 * i;
-      if (c < p.d) p.q[row * p.ldq + c] = (uint8_t)pack2(v[i] * inv, 0.f);
+      const int c = column(g, i);
+      if (c < p.d) p.q[row * p.ldq + c] = (uint8_t)pack2(f[i] * inv, 0.f);
     }
-    if (lane == 0) p.scale[(int64_t)(g0 / GROUP) * p.lds + row] = s;
+    const int grp = warp + g * ANY_WARPS;
+    if (lane == 0 && grp * GROUP < p.d) p.scale[(int64_t)grp * p.lds + row] = s;
+  };
+#pragma unroll
+  for (int g = 0; g < G; ++g) put(g, v[g]);
+  for (int g = G; g < groups; ++g) {  // a thread reads what it wrote itself, or forms it again
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = column(g, i);
+      f[i] = c >= p.d ? 0.f : h ? ld(h + c) : kept<H>(ld(x + c) + (r ? ld(r + c) : 0.f));
+    }
+    put(g, f);
   }
 }
 
 template <typename X, typename H>
 int launch_norm(const NormParams& p, bool vec, cudaStream_t s) {
   if (!vec) {
-    JAGG_CUDA_TRY(launch(rms_norm_fp8_any_kernel<X, H>, dim3((unsigned)p.rows), 256, 0, s, p));
+    const dim3 grid((unsigned)p.rows);
+    const int groups = ceil_div(p.d, GROUP * ANY_WARPS);
+    if (groups == 1)
+      JAGG_CUDA_TRY(launch(rms_norm_fp8_any_kernel<X, H, 1>, grid, 32 * ANY_WARPS, 0, s, p));
+    else if (groups <= 4)
+      JAGG_CUDA_TRY(launch(rms_norm_fp8_any_kernel<X, H, 4>, grid, 32 * ANY_WARPS, 0, s, p));
+    else
+      JAGG_CUDA_TRY(launch(rms_norm_fp8_any_kernel<X, H, 8>, grid, 32 * ANY_WARPS, 0, s, p));
     JAGG_LAUNCHED();
     return JAGG_OK;
   }
@@ -329,41 +369,74 @@ __global__ void __launch_bounds__(C == 1 ? 640 : 512, 1) rms_norm_bwd_kernel(con
   }
 }
 
-// Any width and alignment: element by element, the row read twice, sums over rows in shared memory.
-template <typename Y, typename H>
-__global__ void __launch_bounds__(256) rms_norm_bwd_any_kernel(const NormBwdParams p) {
-  __shared__ float part[8];
-  extern __shared__ float cols[];  // [d] when p.part
+// Rows of any width and alignment, element by element: a CTA of T threads takes a row at a time, a
+// thread the columns t, t + T, ..; E of them and their sums over rows are held in registers, the rest
+// of a longer row is read again for the second pass and summed in shared memory.
+template <typename Y, typename H, int E, int T>
+__global__ void __launch_bounds__(T) rms_norm_bwd_any_kernel(const NormBwdParams p) {
+  __shared__ float part[2][T / 32];
+  extern __shared__ float cols[];  // sums of the columns from T E on
   pdl_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = threadIdx.x;
+  float w[E], dw[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int c = t + T * e;
+    w[e] = c < p.d && p.weight ? load_any(p.weight, p.w_f32, c) : 1.f;
+    dw[e] = 0.f;
+  }
   if (p.part)
-    for (int c = threadIdx.x; c < p.d; c += 256) cols[c] = 0.f;  // a thread's columns are its own throughout
+    for (int c = t + T * E; c < p.d; c += T) cols[c - T * E] = 0.f;  // a thread's columns are its own throughout
+  int turn = 0;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const Y* dy = static_cast<const Y*>(p.dy) + row * p.lddy;
     const H* h = static_cast<const H*>(p.h) + row * p.ldh;
     const H* dh = p.dh ? static_cast<const H*>(p.dh) + row * p.ldg : nullptr;
     H* dx = static_cast<H*>(p.dx) + row * p.ldg;
     const float rstd = p.rstd[row];
-    float sum = 0.f;
-    for (int c = threadIdx.x; c < p.d; c += 256) {
-      const float y = ld(dy + c), xh = ld(h + c) * rstd;
-      if (p.part) cols[c] = fmaf(y, xh, cols[c]);
-      sum = fmaf(y * (p.weight ? load_any(p.weight, p.w_f32, c) : 1.f), xh, sum);
+    float g[E], xh[E], o[E], sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int c = t + T * e;
+      const bool in = c < p.d;
+      g[e] = in ? ld(dy + c) : 0.f;
+      xh[e] = in ? ld(h + c) : 0.f;
+      o[e] = in && dh ? ld(dh + c) : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (t + T * e < p.d) {  // (a column past the row takes no part, whatever rstd is)
+        xh[e] *= rstd;
+        dw[e] = fmaf(g[e], xh[e], dw[e]);
+        g[e] *= w[e];
+        sum = fmaf(g[e], xh[e], sum);
+      }
+    for (int c = t + T * E; c < p.d; c += T) {
+      const float y = ld(dy + c), x = ld(h + c) * rstd;
+      if (p.part) cols[c - T * E] = fmaf(y, x, cols[c - T * E]);
+      sum = fmaf(y * (p.weight ? load_any(p.weight, p.w_f32, c) : 1.f), x, sum);
     }
     sum = warp_sum(sum);
-    __syncthreads();  // the last row's readers are done
-    if (lane == 0) part[warp] = sum;
+    if (lane == 0) part[turn][warp] = sum;
     __syncthreads();
     sum = 0.f;
-    for (int k = 0; k < 8; ++k) sum += part[k];
+    for (int k = 0; k < T / 32; ++k) sum += part[turn][k];
+    turn ^= 1;
     const float mean = sum / (float)p.d;
-    for (int c = threadIdx.x; c < p.d; c += 256) {
-      const float g = ld(dy + c) * (p.weight ? load_any(p.weight, p.w_f32, c) : 1.f), xh = ld(h + c) * rstd;
-      st(dx + c, fmaf(rstd, g - xh * mean, dh ? ld(dh + c) : 0.f));
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (t + T * e < p.d) st(dx + t + T * e, fmaf(rstd, g[e] - xh[e] * mean, o[e]));
+    for (int c = t + T * E; c < p.d; c += T) {
+      const float y = ld(dy + c) * (p.weight ? load_any(p.weight, p.w_f32, c) : 1.f), x = ld(h + c) * rstd;
+      st(dx + c, fmaf(rstd, y - x * mean, dh ? ld(dh + c) : 0.f));
     }
   }
-  if (p.part)
-    for (int c = threadIdx.x; c < p.d; c += 256) p.part[(int64_t)blockIdx.x * p.d + c] = cols[c];
+  if (!p.part) return;
+  float* out = p.part + (int64_t)blockIdx.x * p.d;
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (t + T * e < p.d) out[t + T * e] = dw[e];
+  for (int c = t + T * E; c < p.d; c += T) out[c] = cols[c - T * E];
 }
 
 // dweight (+)= the column sums of part [n, d], in order: 32 columns x 8 row lanes per CTA.
@@ -412,10 +485,21 @@ int launch_norm_bwd(const NormBwdParams& p, bool vec, float* dweight, int accumu
   int ctas;
   if (!vec) {
     ctas = (int)(p.rows < BWD_MAX_CTAS ? p.rows : BWD_MAX_CTAS);
-    auto kernel = rms_norm_bwd_any_kernel<Y, H>;
-    static OncePerDevice once;
-    JAGG_CUDA_TRY(allow_smem(once, kernel, (int)NORM_MAX_D * 4));
-    JAGG_CUDA_TRY(launch(kernel, ctas, 256, p.part ? (size_t)p.d * 4 : 0, s, p));
+    auto any = [&](auto kernel, OncePerDevice& once, int threads, int each) -> int {
+      const int held = threads * each;
+      JAGG_CUDA_TRY(allow_smem(once, kernel, (int)NORM_MAX_D * 4));
+      JAGG_CUDA_TRY(launch(kernel, ctas, threads, p.part && p.d > held ? (size_t)(p.d - held) * 4 : 0, s, p));
+      return JAGG_OK;
+    };
+    static OncePerDevice once[4];
+    if (p.d <= 1024)
+      JAGG_TRY(any(rms_norm_bwd_any_kernel<Y, H, 4, 256>, once[0], 256, 4));
+    else if (p.d <= 2048)
+      JAGG_TRY(any(rms_norm_bwd_any_kernel<Y, H, 4, 512>, once[1], 512, 4));
+    else if (p.d <= 4096)
+      JAGG_TRY(any(rms_norm_bwd_any_kernel<Y, H, 8, 512>, once[2], 512, 8));
+    else
+      JAGG_TRY(any(rms_norm_bwd_any_kernel<Y, H, 16, 512>, once[3], 512, 16));
   } else {
     const int chunks = ceil_div(p.d, 256);
     // A run per thread up to 20 warps, else two.  Two also for many bf16 rows where that keeps 14 warps
@@ -482,8 +566,8 @@ struct Kept8<bf16> {
   }
 };
 
-// A 128 x 128 tile per CTA of 256 threads: thread (c, r) = (t & 15, t >> 4) holds columns 8 c .. + 7 of
-// the rows r, r + 16, .., r + 112, so a row group is one half warp's and a column group is 16
+// A 128 x 128 tile per CTA of 256 threads: thread (c, r) = (t & 15, t >> 4) holds columns 8 c .. + 7
+// (element by element, without VEC: c, c + 16, ..) of the rows r, r + 16, .., r + 112, so a row group is one half warp's and a column group is 16
 // threads' eight rows each, joined in shared memory.  K: what a thread keeps its elements as (bf16
 // only where no multipliers change them).
 template <typename X, typename K, bool VEC>
@@ -492,8 +576,11 @@ __global__ void __launch_bounds__(256, sizeof(K) == 2 ? (VEC ? 4 : 3) : 2) quant
   __shared__ float whole[8];
   pdl_wait();
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
-  const int64_t row0 = (int64_t)blockIdx.y * GROUP, col0 = (int64_t)blockIdx.x * GROUP + 8 * c;
-  const int live = (int)(p.cols - col0 < 0 ? 0 : p.cols - col0 < 8 ? p.cols - col0 : 8);  // columns of this thread
+  constexpr int STEP = VEC ? 1 : 16;  // between a thread's columns: element by element, 16 lanes take neighbours
+  const int at0 = VEC ? 8 * c : c;    // the thread's first column in the tile
+  const int64_t row0 = (int64_t)blockIdx.y * GROUP, col0 = (int64_t)blockIdx.x * GROUP + at0;
+  const int64_t left = p.cols - col0;
+  const int live = left <= 0 ? 0 : left >= 8 * STEP ? 8 : (int)((left + STEP - 1) / STEP);  // columns of this thread
   Kept8<K> v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -513,7 +600,7 @@ __global__ void __launch_bounds__(256, sizeof(K) == 2 ? (VEC ? 4 : 3) : 2) quant
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (j < live) f[j] = ld(x + j);
+            if (j < live) f[j] = ld(x + j * STEP);
         }
       }
 #pragma unroll
@@ -535,7 +622,7 @@ __global__ void __launch_bounds__(256, sizeof(K) == 2 ? (VEC ? 4 : 3) : 2) quant
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (j >= live) continue;
-        const float m = load_any(p.col_mul, p.col_f32, col0 + j);
+        const float m = load_any(p.col_mul, p.col_f32, col0 + j * STEP);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           if (row0 + r + 16 * i < p.rows) v[i].v[j] *= m;
@@ -550,7 +637,7 @@ __global__ void __launch_bounds__(256, sizeof(K) == 2 ? (VEC ? 4 : 3) : 2) quant
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (j < live) at[j] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+        if (j < live) at[j * STEP] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
     }
   };
   if (p.row.q) {
@@ -577,7 +664,7 @@ __global__ void __launch_bounds__(256, sizeof(K) == 2 ? (VEC ? 4 : 3) : 2) quant
       float a = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) a = amax(a, v[i].at(j));
-      peak[r][8 * c + j] = a;
+      peak[r][at0 + j * STEP] = a;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i].forget();
@@ -594,7 +681,7 @@ __global__ void __launch_bounds__(256, sizeof(K) == 2 ? (VEC ? 4 : 3) : 2) quant
     __syncthreads();
     float inv[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) inv[j] = peak[0][8 * c + j];
+    for (int j = 0; j < 8; ++j) inv[j] = peak[0][at0 + j * STEP];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t row = row0 + r + 16 * i;

@@ -89,6 +89,15 @@ def test_product_refusals(jg, change, word):
     _refused(jg, jg.lib().jagg_gemm_fp8(ctypes.byref(d), None), -1, "jagg_gemm_fp8", word)
 
 
+@pytest.mark.parametrize("plan,change,word", [
+    ((64, 0, 1, 0), {}, "pair tiles"), ((0, 128, 0, 0), {}, "splits"), ((0, 128, 9, 0), {}, "splits"), ((0, 128, 4, 0), {}, "splits"),
+    ((0, 64, 1, 0), {}, "tiles"), ((0, 128, 1, 1), {}, "tiles"), ((0, 16, 1, 1), dict(a_trans=1, lda=16), "tiles"),
+    ((0, 128, 1, 0), dict(K=0), "empty"), ((256, 0, 1, 0), dict(M=0), "empty"), ((256, 0, 1, 0), dict(A=None), "A needs")])
+def test_product_by_kernel_refusals(jg, plan, change, word):
+    d = jg.GemmFp8Desc(**dict(GEMM, **change))
+    _refused(jg, jg.lib().jagg_test_gemm_fp8(ctypes.byref(d), *plan, None), -1, "jagg_test_gemm_fp8", word)
+
+
 def test_product_without_descriptor(jg):
     _refused(jg, jg.lib().jagg_gemm_fp8(None, None), -1, "null")
 

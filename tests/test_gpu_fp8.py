@@ -121,8 +121,8 @@ def test_norm_of_no_rows_launches_nothing():
 # ------------------------------------------------------------------ norm backward
 @pytest.mark.parametrize("y,h", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32"), ("f32", "bf16")])
 @pytest.mark.parametrize("rows,d,pad", [(1, 1, 0), (3, 127, 0), (17, 128, 0), (2, 129, 1), (9, 256, 8), (700, 768, 0),
-                                        (1300, 300, 0), (5, 1536, 0), (3, 4096, 0), (620, 5120, 0), (2, 8192, 0),
-                                        (3, 8200, 0), (2, 32768, 0)])
+                                        (1300, 300, 0), (2500, 512, 0), (5, 1536, 0), (3, 1537, 0), (3, 4096, 0), (3, 4001, 0),
+                                        (620, 5120, 0), (2, 5121, 0), (2, 8192, 0), (3, 8200, 0), (2, 32768, 0), (1, 32767, 0)])
 def test_norm_backward(rows, d, pad, y, h):
     dy = _pitched(_rand(rows, d, dtype=DT[y], seed=1), pad)
     hs = _pitched(_rand(rows, d, dtype=DT[h], scale=2.0, seed=2), pad)
@@ -275,6 +275,41 @@ def test_product(M, N, K, a_trans, b_trans, b_form, out):
     jg.gemm_fp8(a, sa, b, sb, c, a_trans=bool(a_trans), b_trans=bool(b_trans))
     check_product(c, va.t() if a_trans else va, vb.t() if b_trans else vb)
     assert (buf[M:] == 5.0).all() and (buf[:M, N:] == 5.0).all()
+
+
+PLANS = [dict(pair=256), dict(pair=128), dict(nt=128, splits=1), dict(nt=128, splits=3), dict(nt=128, splits=8),
+         dict(nt=16, splits=1, swap=True), dict(nt=32, splits=2, swap=True), dict(nt=64, splits=5, swap=True)]
+
+
+@pytest.mark.parametrize("plan", range(len(PLANS)))
+@pytest.mark.parametrize("a_trans,b_trans,b_form", [(0, 0, "block"), (0, 0, "row"), (0, 1, "block"), (0, 1, "col"),
+                                                    (1, 0, "row"), (1, 0, "block"), (1, 1, "col"), (1, 1, "block")])
+def test_product_by_every_kernel(plan, a_trans, b_trans, b_form):
+    """Every kernel and tile on whole and ragged tiles, more tiles than CTA pairs, one k-block and more
+    than 32 of them (the block scales' batch), outputs that TMA stores serve (rows of 16 bytes) and that
+    they do not, with bias and accumulation."""
+    plan = PLANS[plan]
+    if plan.get("swap") and a_trans:
+        pytest.skip("rows of A as accumulator columns need a K-major A")
+    few = plan.get("swap") or plan.get("splits", 1) > 1
+    sizes = [(1, 1, 1024), (70, 130, 1030), (256, 256, 1024)] + ([] if few else [(600, 777, 128), (300, 520, 4800), (2600, 4104, 256)])
+    for M, N, K in sizes:
+        a, sa, va = _operand(*((K, M) if a_trans else (M, K)), "col" if a_trans else "row", 1)
+        b, sb, vb = _operand(*((K, N) if b_trans else (N, K)), b_form, 2, pad=16)
+        va, vb = va.t() if a_trans else va, vb.t() if b_trans else vb
+        bias = _rand(N, seed=7)
+        kw = dict(a_trans=bool(a_trans), b_trans=bool(b_trans), **plan)
+        for out, pad in (("bf16", 5), ("bf16", (8 - N) % 8 + 8), ("f32", 3), ("f32", (4 - N) % 4 + 4)):
+            buf = torch.full((M + 1, N + pad), 5.0, dtype=DT[out], device="cuda")
+            c = buf[:M, :N]
+            jg.test_gemm_fp8(a, sa, b, sb, c, bias=bias, **kw)
+            check_product(c, va, vb, bias=bias)
+            if out == "f32":
+                start = c.clone()
+                jg.test_gemm_fp8(a, sa, b, sb, c, accumulate=True, **kw)
+                check_product(c, va, vb, start=start)
+            assert (buf[M:] == 5.0).all() and (buf[:M, N:] == 5.0).all()
+    assert jg.device_status() == 0
 
 
 @pytest.mark.parametrize("M,N,K,pad", [(1, 96, 512, 0), (5, 640, 1024, 0), (40, 130, 300, 3), (200, 136, 520, 0), (300, 261, 700, 1),
