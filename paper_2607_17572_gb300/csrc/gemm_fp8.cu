@@ -236,14 +236,14 @@ __global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
       if (!p.p_block) s *= ptx::ld_shared(ps);
       fp8::named_sync(1 + a * (Cfg::EW / 4) + sl, 160);  // the watcher has seen the accumulator complete
       ptx::tc_fence_after();
-      fp8::scaled_add<CW, QVEC, (CW < 32 ? 16 : 32)>(acc, t0 + a * NT, s, qs);
-      ptx::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(&tempty[a]);
+      fp8::scaled_add<CW, QVEC, (CW < 32 ? 16 : 32)>(acc, t0 + a * NT, s, qs, [&] {
+        if (lane == 0) ptx::mbar_arrive(&tempty[a]);
+      });
       if (++a == F_ACCS) a = 0;
       ps += F_ROWS * 4;
       qs += NT * 4;
       if (at % SCALE_KB == SCALE_KB - 1) {
+        __syncwarp();  // every lane has used its scales
         if (lane == 0) ptx::mbar_arrive(&sempty[slots & 1]);
         ++slots;
       }
@@ -398,12 +398,14 @@ int launch_f8(const GemmFp8Args& g, int splits, cudaStream_t s) {
   return JAGG_OK;
 }
 
-// Microseconds that a k-block takes, by kernel and tile, and what a tile and a launch take besides;
-// measured on 4096 x 4096 weights with 128 to 8192 rows, and on weight gradients of that size.  B's
-// vector scales cost a multiplication per element more than block scales.
-constexpr double US_LAUNCH = 2.8, US_TILE_ONE = 1.5, US_TILE_PAIR = 2.0, US_JOIN = 1.0;
-double us_one(int nt, bool qvec) { return nt <= 16 ? 0.15 : nt == 32 ? 0.22 : nt == 64 ? 0.4 : qvec ? 0.66 : 0.47; }
-double us_pair(int bn, bool qvec) { return bn == 256 ? (qvec ? 0.78 : 0.46) : qvec ? 0.53 : 0.33; }
+// Microseconds that a k-block takes, by kernel and tile, and what a tile and a launch take besides,
+// fitted to products of 1 to 8192 rows with 512 to 8192 along K: 4864 x 4096 x 4096 takes 66 us in pair tiles
+// of 256 columns, 93 in tiles of 128 and 115 in single CTAs, 512 x 4096 x 4096 17.7, 14.6 and 15.0,
+// 128 x 4096 x 4096 split four ways 9.0, against 14.0 for either unsplit.  B's vector scales cost a
+// multiplication per element more than block scales.
+constexpr double US_LAUNCH = 2.0, US_TILE_ONE = 2.5, US_TILE_PAIR = 2.2, US_JOIN = 0.5;
+double us_one(int nt, bool qvec) { return nt == 16 ? 0.165 : nt == 32 ? 0.28 : nt == 64 ? 0.42 : qvec ? 0.5 : 0.35; }
+double us_pair(int bn, bool qvec) { return bn == 256 ? (qvec ? 0.67 : 0.44) : qvec ? 0.48 : 0.31; }
 
 // CTAs that run at one time in clusters of n: a cluster has to fit into the SMs of one GPC, so that up
 // to an eighth of the machine stays idle (18 tiles split 8 ways, 144 CTAs, take two turns: 15.6 us,

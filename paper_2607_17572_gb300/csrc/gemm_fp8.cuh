@@ -59,35 +59,47 @@ __device__ __forceinline__ void named_arrive(int id, int threads) {
   asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
+// (x, y) += (a, b) f, as one paired instruction.
+__device__ __forceinline__ void add2(float& x, float& y, uint32_t a, uint32_t b, float2 f) {
+  asm volatile(
+      "{\n\t.reg .b64 d, c, q;\n\t"
+      "mov.b64 d, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tmov.b64 c, {%0, %1};\n\t"
+      "fma.rn.f32x2 c, d, q, c;\n\tmov.b64 {%0, %1}, c;\n\t}"
+      : "+f"(x), "+f"(y)
+      : "r"(a), "r"(b), "f"(f.x), "f"(f.y));
+}
+
 // acc[j] += s d[j] (q[j]) over CW columns of an accumulator, from tensor-memory address `t`: the inner
 // sum of one group times its two scales.  s: the row's scale (times the columns' where they share one);
 // q: address of the columns' scales in shared memory when QVEC.
 //
-// One f32 instruction per element: the paired form takes half as many, and as many moves again to
-// form its register pairs from the loaded words.
-template <int CW, bool QVEC, int STEP>
-__device__ __forceinline__ void scaled_add(float (&acc)[CW], uint32_t t, float s, uint32_t q) {
+// `read()` is called by the warp once all of its columns have been read, before the last are added: the
+// accumulator goes back to the tensor core that much earlier.
+template <int CW, bool QVEC, int STEP, class Read>
+__device__ __forceinline__ void scaled_add(float (&acc)[CW], uint32_t t, float s, uint32_t q, Read read) {
 #pragma unroll
   for (int c = 0; c < CW; c += STEP) {
     uint32_t r[STEP];
-    if constexpr (STEP == 8)
-      ptx::tmem_ld_32x32b_x8(t + c, r);
-    else if constexpr (STEP == 16)
+    if constexpr (STEP == 16)
       ptx::tmem_ld_32x32b_x16(t + c, r);
     else
       ptx::tmem_ld_32x32b_x32(t + c, r);
     ptx::tmem_ld_wait();
+    if (c + STEP >= CW) {
+      ptx::tc_fence_before();
+      __syncwarp();
+      read();
+    }
 #pragma unroll
     for (int j = 0; j < STEP; j += 4) {
-      float4 f = make_float4(s, s, s, s);
+      float2 f = make_float2(s, s), g = f;
       if constexpr (QVEC) {
-        f = ptx::ld_shared_v4(q + (c + j) * 4);
-        f.x *= s; f.y *= s; f.z *= s; f.w *= s;
+        const float4 v = ptx::ld_shared_v4(q + (c + j) * 4);
+        f = ptx::mul2(make_float2(v.x, v.y), f);
+        g = ptx::mul2(make_float2(v.z, v.w), g);
       }
-      acc[c + j] = fmaf(__uint_as_float(r[j]), f.x, acc[c + j]);
-      acc[c + j + 1] = fmaf(__uint_as_float(r[j + 1]), f.y, acc[c + j + 1]);
-      acc[c + j + 2] = fmaf(__uint_as_float(r[j + 2]), f.z, acc[c + j + 2]);
-      acc[c + j + 3] = fmaf(__uint_as_float(r[j + 3]), f.w, acc[c + j + 3]);
+      add2(acc[c + j], acc[c + j + 1], r[j], r[j + 1], f);
+      add2(acc[c + j + 2], acc[c + j + 3], r[j + 2], r[j + 3], g);
     }
   }
 }
