@@ -439,25 +439,23 @@ __global__ void __launch_bounds__(T) rms_norm_bwd_any_kernel(const NormBwdParams
   for (int c = t + T * E; c < p.d; c += T) out[c] = cols[c - T * E];
 }
 
-// dweight (+)= the column sums of part [n, d], in order: 32 columns x 8 row lanes per CTA.
-__global__ void __launch_bounds__(256) dweight_kernel(const float* part, int n, int d, float* dweight, int accumulate) {
-  __shared__ float red[8][32];
+// dweight (+)= the column sums of part [n, d], in order: 32 columns x 32 row lanes per CTA, so that a
+// column's 152 rows (a CTA per SM) are five loads in flight per thread.
+__global__ void __launch_bounds__(1024) dweight_kernel(const float* part, int n, int d, float* dweight, int accumulate) {
+  __shared__ float red[32][33];
   pdl_wait();
   const int lane = threadIdx.x & 31, r0 = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + lane;
   float s = 0.f;
   if (c < d) {
 #pragma unroll 8
-    for (int r = r0; r < n; r += 8) s += part[(int64_t)r * d + c];
+    for (int r = r0; r < n; r += 32) s += part[(int64_t)r * d + c];
   }
   red[r0][lane] = s;
   __syncthreads();
-  if (r0 == 0 && c < d) {
-    s = 0.f;
-#pragma unroll
-    for (int r = 0; r < 8; ++r) s += red[r][lane];
-    dweight[c] = accumulate ? dweight[c] + s : s;
-  }
+  s = warp_sum(red[lane][r0]);  // warp r0 joins column r0
+  const int out = blockIdx.x * 32 + r0;
+  if (lane == 0 && out < d) dweight[out] = accumulate ? dweight[out] + s : s;
 }
 
 // Row slots of `warps` warps each: CTAs of about 16 warps, one per SM, as many CTAs as there are rows
@@ -522,7 +520,7 @@ int launch_norm_bwd(const NormBwdParams& p, bool vec, float* dweight, int accumu
   }
   JAGG_LAUNCHED();
   if (p.part) {
-    JAGG_CUDA_TRY(launch(dweight_kernel, ceil_div(p.d, 32), 256, 0, s, (const float*)p.part, ctas, p.d, dweight,
+    JAGG_CUDA_TRY(launch(dweight_kernel, ceil_div(p.d, 32), 1024, 0, s, (const float*)p.part, ctas, p.d, dweight,
                          accumulate));
     JAGG_LAUNCHED();
   }
