@@ -358,7 +358,8 @@ int grad_reduce(const float* a, const float* b, int64_t P, float alpha, float* a
  *   q, scale  device, row groups of [rows, d]
  *   rstd      device [rows] f32, 1 / sqrt(mean(h^2) + eps), or NULL
  * 1 <= d <= 32768.  x, residual and h_out need the alignment of their elements only; with 16-byte
- * aligned rows and d a multiple of 8 a faster kernel runs. */
+ * aligned rows and d a multiple of 8 a faster kernel runs.  A row whose sum of squares leaves f32's
+ * range has 1 / sqrt 0, and zeros in q; one of zeros needs eps > 0.  */
 int jagg_rms_norm_fp8(const void* x, int x_dtype, int64_t ldx, const void* residual, int h_dtype, int64_t ldh,
                       const void* weight, int w_dtype, int64_t rows, int64_t d, float eps, void* h_out, uint8_t* q,
                       int64_t ldq, float* scale, int64_t lds, float* rstd, cudaStream_t stream);
@@ -384,7 +385,7 @@ int jagg_rms_norm_bwd(const void* dy, int dy_dtype, int64_t lddy, const void* h,
  * the three forms, all from one read of x.  A form whose q is NULL is not written.
  * With x = h, row_mul = rstd and col_mul = weight the norm's output is formed again, for the
  * weight gradient (which takes column groups).
- *   x        device [rows, cols] x_dtype, row pitch ldx
+ *   x        device [rows, cols] x_dtype, row pitch ldx; at most 65535 * 128 rows
  *   row_mul  device [rows] f32;  col_mul  device [cols] col_mul_dtype                     */
 typedef struct jagg_fp8_out {
   uint8_t* q;
@@ -434,8 +435,9 @@ int jagg_gemm_fp8(const jagg_gemm_fp8_desc* desc, cudaStream_t stream);
  * jagg_grad_norm writes norm to norm_out (device f32 [1]).
  * jagg_grad_clip writes {norm, coef} to norm_out (device f32 [2]) and out[i] = coef grads[i] (NULL: in
  * place; an out tensor is its gradient's own buffer or does not overlap any gradient).  Where coef
- * is 1 nothing is written in place.  A NaN or infinite gradient makes the norm that: NaN leaves NaN
- * in every output, infinity leaves 0 in every finite element and NaN in the infinite ones.
+ * is 1 nothing is written in place.  No tensor may appear twice or overlap another.  A NaN or infinite
+ * gradient makes the norm that: NaN leaves NaN in every output, infinity leaves 0 in every finite
+ * element and NaN in the infinite ones.  An infinite max_norm clips nothing.
  *   ws    device workspace of >= jagg_grad_clip_workspace_bytes(count) bytes, 8-byte aligned */
 int64_t jagg_grad_clip_workspace_bytes(int count);
 int jagg_grad_norm(const void* const* grads, const int64_t* numel, int count, int dtype, float* norm_out, void* ws,

@@ -166,7 +166,8 @@ __global__ void __launch_bounds__(CLIP_THREADS)
   pdl_wait();
   const double norm = sqrt(total_of(part, parts, red));
   const double below = norm + eps;
-  const double ratio = below == 0.0 ? 1.0 : max_norm / below;  // nothing to clip where all gradients are 0
+  // nothing to clip where all gradients are 0, or without a limit
+  const double ratio = below == 0.0 || (isinf(max_norm) && !isnan(norm)) ? 1.0 : max_norm / below;
   const float coef = ratio >= 1.0 ? 1.f : (float)ratio;        // a NaN stays one
   if (write_norm && blockIdx.x == 0 && threadIdx.x == 0) {
     out2[0] = (float)norm;

@@ -103,6 +103,30 @@ def test_zero_and_non_finite_gradients():
     assert out.isnan().all() and all(t.isnan().all() for t in z)
 
 
+def test_no_limit():
+    _, ts = _tensors([100, 9000], torch.float32)
+    before = [t.clone() for t in ts]
+    out, ws = torch.empty(2, device="cuda"), _ws(2)
+    jg.grad_clip(ts, float("inf"), out, ws)
+    assert out[1].item() == 1.0 and all(torch.equal(t, b) for t, b in zip(ts, before))
+    ts[1][7] = float("inf")
+    jg.grad_clip(ts, float("inf"), out, ws)
+    assert out.tolist() == [float("inf"), 1.0] and torch.equal(ts[0], before[0])
+
+
+def test_more_than_2_31_elements():
+    """Offsets beyond 32 bits: the first, some middle and the last elements of one tensor."""
+    n = 2**31 + 12345
+    g = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty(2, device="cuda")
+    jg.grad_clip([g], 1.0, out, _ws(1))
+    ref = float(n) ** 0.5
+    assert abs(out[0].item() / ref - 1) <= 20 * U
+    want = torch.tensor(1.0 / ref, dtype=torch.float64).to(torch.bfloat16)
+    for part in (g[:3], g[2**31 - 3:2**31 + 3], g[-3:]):
+        assert (part.cpu() == want).all()
+
+
 def test_clip_to_zero_and_no_tensors():
     _, ts = _tensors([100, 9000], torch.float32)
     out, ws = torch.empty(2, device="cuda"), _ws(2)
