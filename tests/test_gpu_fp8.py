@@ -394,6 +394,45 @@ def test_product_keeps_f32_across_groups(M):
     check_product(c, held(a, sa, "row"), held(b, sb, "block"))
 
 
+# ------------------------------------------------------------------ offsets beyond 32 bits
+def test_matrices_of_more_than_2_31_elements():
+    """The norm, its backward, quantisation and a product whose outputs have more than 2^31 elements: their
+    last rows equal those of a small call on the same rows, bit for bit where the kernels do not sum
+    over rows."""
+    rows, d, tail = 2**31 // 4096 + 200, 4096, 200
+    x = torch.randn(tail, d, device="cuda").bfloat16()
+    big = torch.zeros(rows, d, dtype=torch.bfloat16, device="cuda")
+    big[-tail:] = x
+    (q, s), (q1, s1) = jg.fp8_buffers(rows, d, "row"), jg.fp8_buffers(tail, d, "row")
+    r, r1 = torch.empty(rows, device="cuda"), torch.empty(tail, device="cuda")
+    h = torch.empty_like(big)
+    jg.rms_norm_fp8(big, q, s, h_out=h, rstd=r)
+    jg.rms_norm_fp8(x, q1, s1, rstd=r1)
+    assert torch.equal(h[-tail:], x) and torch.equal(r[-tail:], r1) and torch.equal(s[:, -tail:], s1)
+    assert torch.equal(q[-tail:].view(torch.uint8), q1.view(torch.uint8))
+    dx1 = torch.empty_like(x)
+    jg.rms_norm_bwd(x, x, r1, dx1)
+    jg.rms_norm_bwd(big, big, r, h)
+    # (few and many rows may be held by different numbers of threads: sums in another order)
+    assert ((h[-tail:].double() - dx1.double()).abs() <= 2 * half_step(torch.bfloat16) * dx1.double().abs() + 1e-5).all()
+    del h
+    jg.quantize_fp8(big, row=(q, s))
+    jg.quantize_fp8(x, row=(q1, s1))
+    assert torch.equal(q[-tail:].view(torch.uint8), q1.view(torch.uint8)) and torch.equal(s[:, -tail:], s1)
+    w, sw = jg.fp8_buffers(d, d, "block")
+    jg.quantize_fp8(torch.randn(d, d, device="cuda"), block=(w, sw))
+    for n in (d, d - 4):  # an output that TMA stores, and one that it does not
+        wn, swn = w[:n], sw
+        c, c1 = torch.empty(rows, n, dtype=torch.bfloat16, device="cuda"), torch.empty(tail, n, dtype=torch.bfloat16, device="cuda")
+        jg.test_gemm_fp8(q, s, wn, swn, c, pair=256)
+        jg.test_gemm_fp8(q1, s1, wn, swn, c1, pair=256)
+        assert torch.equal(c[-tail:], c1)
+        jg.test_gemm_fp8(q, s, wn, swn, c, splits=1)
+        jg.test_gemm_fp8(q1, s1, wn, swn, c1, splits=1)
+        assert torch.equal(c[-tail:], c1)
+    assert jg.device_status() == 0
+
+
 # ------------------------------------------------------------------ together, and how calls are made
 def _layer(M, d, n, seed):
     t = dict(x=_rand(M, d, dtype=torch.bfloat16, seed=seed), r=_rand(M, d, seed=seed + 1), w=_rand(d, scale=0.2, seed=seed + 2) + 1,
