@@ -62,10 +62,10 @@ def parse():
     p.add_argument("--quick", action="store_true", help="skip the full-W, e2e and CPU legs")
     p.add_argument("--G", type=int, default=0,
                    help="override the workload's group size (small cases for profiler captures)")
-    p.add_argument("--kernel", choices=["attention_bwd", "attention_fwd", "gemm", "hbm"], default=None,
+    p.add_argument("--kernel", choices=["attention_bwd", "attention_fwd", "gemm", "gemm_fp8", "hbm"], default=None,
                    help="time one kernel family alone on the workload's shapes instead of the step")
     p.add_argument("--product", default="all",
-                   help="for --kernel gemm: one of the block's backward products (gemm_products: DiT fc2_dx, "
+                   help="for --kernel gemm and gemm_fp8: one of the block's backward products (gemm_products: DiT fc2_dx, "
                         "fc1_dx, qkv_dx, proj_dx, fc2_dw, fc1_dw, qkv_dw, proj_dw; MMDiT lin2_dx_o, lin2_dx_u, "
                         "lin1_dx, lin2_dw, lin1_dw and the img_ products of a double block) or all")
     p.add_argument("--rows", type=int, default=0, help="sequences per call for --kernel (default 2G)")
@@ -1187,6 +1187,57 @@ def run_kernel_gemm(args):
                       "products": out}), flush=True)
 
 
+def run_kernel_gemm_fp8(args):
+    """The same products (and the forward product of each input gradient's weight) of 8-bit operands:
+    activations and their gradients with a scale for each row and 128 columns (for a weight gradient:
+    column and 128 tokens), weights for each 128 x 128 block; outputs bf16, weight gradients f32.
+    Timed with CUDA events over the timed calls."""
+    import paper_2607_17572_gb300 as jg
+    wl = workload(args)
+    dev = torch.device("cuda", torch.cuda.current_device())
+    rows = (args.rows or 2 * wl.G * (wl.T // wl.W)) * wl.n_tok
+    prods = {}
+    for name, (M, N, K, a_mn, b_mn, _) in gemm_products(wl, rows).items():
+        if not a_mn:
+            prods[name[:-2] + "fwd" if name.endswith("dx") else name.replace("_dx_", "_fwd_")] = (M, K, N, False, False)
+        prods[name] = (M, N, K, a_mn, b_mn)
+    names = list(prods) if args.product == "all" else [args.product]
+    gen = torch.Generator(device=dev).manual_seed(synth.NOISE_SEED)
+    burst, sustained, hbm, src = peaks()
+
+    def operand(r, c, form):
+        q = jg.fp8_buffers(r, c, form, dev)
+        jg.quantize_fp8(torch.randn(r, c, device=dev, generator=gen).bfloat16(), **{form: q})
+        return q
+    out = {}
+    for name in names:
+        M, N, K, a_mn, b_mn = prods[name]
+        a = operand(K, M, "col") if a_mn else operand(M, K, "row")
+        b = operand(*((K, N) if b_mn else (N, K)), "col" if a_mn else "block")
+        C = torch.empty(M, N, device=dev, dtype=torch.float32 if a_mn else torch.bfloat16)
+        call = lambda: jg.gemm_fp8(*a, *b, C, a_trans=a_mn, b_trans=b_mn)
+        for _ in range(args.warmup):
+            call()
+        torch.cuda.synchronize()
+        stream = torch.cuda.current_stream()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        torch.cuda.profiler.start()
+        e0.record(stream)
+        for _ in range(args.steps):
+            call()
+        e1.record(stream)
+        torch.cuda.synchronize()
+        torch.cuda.profiler.stop()
+        ms = e0.elapsed_time(e1) / args.steps
+        tf = 2.0 * M * N * K / (ms / 1000.0) / 1e12
+        out[name] = {"M": M, "N": N, "K": K, "ms_per_call": ms, "tflops": tf, "of_bf16_burst": tf / burst}
+        del a, b, C
+        torch.cuda.empty_cache()
+    print(json.dumps({"kernel": "gemm_fp8", "workload": describe(wl), "rows": rows, "steps": args.steps,
+                      "peak": {"tflops": burst, "source": f"bf16_tflops (burst) of {src} peaks"},
+                      "products": out}), flush=True)
+
+
 def run_kernel_hbm(args):
     """The bandwidth-bound kernels of the joint VJP alone at the workload's per-window shapes
     (rows = 2G sequences of one window by default) on random operands, each timed by the
@@ -1194,7 +1245,9 @@ def run_kernel_hbm(args):
     copy bandwidth: the LayerNorm + modulation and gate backward (a single block's rows), the
     QK-norm + RoPE forward and backward, the bias column sums (a single block's lin1 output
     gradient), the step signals with the fused aggregation, grad_reduce (a 256 M-parameter
-    slice: the norm and a dot with a second gradient).  Every operand a few hundred MB."""
+    slice: the norm and a dot with a second gradient), the clip of that slice, and of the 8-bit
+    projections the norm, its backward and the quantisation of a gradient.  Every operand a few
+    hundred MB."""
     import paper_2607_17572_gb300 as jg
     wl = workload(args)
     dev = torch.device("cuda", torch.cuda.current_device())
@@ -1280,6 +1333,21 @@ def run_kernel_hbm(args):
     out3 = torch.zeros(3, **f64)
     gws = jg.alloc_bytes(jg.grad_reduce_workspace_bytes(P), dev)
     run("grad_reduce_dot", "grad_reduce", lambda: jg.grad_reduce(ga, gb, out3=out3, ws=gws))
+    norm = torch.empty(2, **f)
+    cws = jg.alloc_bytes(jg.grad_clip_workspace_bytes(1), dev)
+    run("grad_clip", "grad_clip", lambda: jg.grad_clip([ga], 1.0, norm, cws, out=[gb]))
+    del ga, gb
+    torch.cuda.empty_cache()
+    # the norm in front of an 8-bit projection, its backward, and the gradient for both gradient products
+    x = torch.randn(M, d, **f, generator=gen).to(bf)
+    res, wn, rstd = torch.randn(M, d, **f, generator=gen), torch.ones(d, **f), torch.empty(M, **f)
+    h, q = torch.empty_like(res), jg.fp8_buffers(M, d, "row", dev)
+    run("rms_norm_fp8", "rms_norm_fp8", lambda: jg.rms_norm_fp8(x, *q, residual=res, weight=wn, h_out=h, rstd=rstd))
+    dw, nws = torch.empty(d, **f), jg.alloc_bytes(jg.rms_norm_bwd_workspace_bytes(M, d), dev)
+    run("rms_norm_bwd", "rms_norm_bwd",
+        lambda: jg.rms_norm_bwd(x, h, rstd, res, weight=wn, dh=res, dweight=dw, ws=nws))
+    qc = jg.fp8_buffers(M, d, "col", dev)
+    run("quantize_fp8", "quantize_fp8", lambda: jg.quantize_fp8(x, row=q, col=qc))
     print(json.dumps({"kernel": "hbm", "workload": describe(wl), "rows": M, "sequences": seqs, "steps": args.steps,
                       "peak": {"hbm_gbs": hbm, "source": f"hbm_gbs of {src} peaks"}, "kernels": out}), flush=True)
 
@@ -1293,6 +1361,9 @@ def main():
     elif args.kernel == "gemm":
         if rank == 0:
             run_kernel_gemm(args)
+    elif args.kernel == "gemm_fp8":
+        if rank == 0:
+            run_kernel_gemm_fp8(args)
     elif args.kernel == "hbm":
         if rank == 0:
             run_kernel_hbm(args)
