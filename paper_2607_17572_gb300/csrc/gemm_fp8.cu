@@ -38,6 +38,7 @@ using fp8::SCALE_KB;
 constexpr int F_ROWS = 128;                  // P rows of a tile
 constexpr int F_TILE = F_ROWS * GROUP;       // bytes of a whole operand tile of a k-block
 constexpr int F_ACCS = 4;                    // accumulators in tensor memory
+constexpr int F_BARS = F_ACCS + 2;           // sets of named barriers (fp8::named_arrive)
 constexpr int F_MAX_STAGES = 10;
 constexpr int F_MAX_SPLITS = 8;              // portable cluster size
 constexpr int F_SMEM = 200 * 1024;
@@ -148,6 +149,8 @@ __global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
           ptx::tma_load_2d(sP + F_TILE, &maps.q, &full[stage], q0, kb * GROUP);
         else
           ptx::tma_load_2d(sP + F_TILE, &maps.q, &full[stage], kb * GROUP, q0);
+        issued |= 1u << stage;
+        issued_parity = (issued_parity & ~(1u << stage)) | (phase << stage);
         if ((kb - kb0) % SCALE_KB == 0) {
           const uint32_t slot = slots & 1;
           if (!ptx::mbar_wait(&sempty[slot], ((slots >> 1) & 1) ^ 1)) { abort_flag = 1; break; }
@@ -156,15 +159,12 @@ __global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
           if (QVEC) ptx::tma_load_2d(qscale[slot], &maps.qs, &sfull[slot], q0, kb);
           ++slots;
         }
-        issued |= 1u << stage;
-        issued_parity = (issued_parity & ~(1u << stage)) | (phase << stage);
         if (++stage == Cfg::STAGES) { stage = 0; phase ^= 1; }
       }
-      if (abort_flag) {  // after a give-up: loads already issued land before shared memory goes away
-        for (int s = 0; s < Cfg::STAGES; ++s)
-          if (issued & (1u << s)) ptx::mbar_wait(&full[s], (issued_parity >> s) & 1u);
-        for (uint32_t n = slots > 2 ? slots - 2 : 0; n < slots; ++n) ptx::mbar_wait(&sfull[n & 1], (n >> 1) & 1);
-      }
+      // every load has landed before shared memory is used again
+      for (int s = 0; s < Cfg::STAGES; ++s)
+        if (issued & (1u << s)) ptx::mbar_wait(&full[s], (issued_parity >> s) & 1u);
+      for (uint32_t n = slots > 2 ? slots - 2 : 0; n < slots; ++n) ptx::mbar_wait(&sfull[n & 1], (n >> 1) & 1);
     }
   } else if (warp == 1) {
     if (ptx::elect_one()) {
@@ -198,16 +198,23 @@ __global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
     }
   } else if (warp == 2) {
     // ---------------- watcher
-    int a = 0;
+    int a = 0, bar = 0;
     uint32_t a_phase = 0;
-    bool alive = true;  // after a give-up the epilogue is let go without data, so that it ends
+    bool ok = true;
     for (int kb = kb0; kb < kb1; ++kb) {
-      if (alive) alive = ptx::mbar_wait(&tfull[a], a_phase);
-      if (!alive) abort_flag = 1;
-      __syncwarp();
+      const int id = 1 + bar * (Cfg::EW / 4);
+      if (ok) {
+        ok = ptx::mbar_wait(&tfull[a], a_phase);
+        if (!ok) abort_flag = 1;
+        __syncwarp();
 #pragma unroll
-      for (int sl = 0; sl < Cfg::EW / 4; ++sl) fp8::named_arrive(1 + a * (Cfg::EW / 4) + sl, 160);
+        for (int sl = 0; sl < Cfg::EW / 4; ++sl) fp8::named_arrive(id + sl, 160);
+        ok = __all_sync(0xffffffffu, ok);
+      } else {
+        for (int sl = 0; sl < Cfg::EW / 4; ++sl) fp8::named_sync(id + sl, 160);
+      }
       if (++a == F_ACCS) { a = 0; a_phase ^= 1; }
+      if (++bar == F_BARS) bar = 0;
     }
   } else if (warp >= 4) {
     // ---------------- epilogue: thread = P row, CW columns of Q
@@ -218,7 +225,7 @@ __global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
     const float* bs = p.block + (int64_t)((p.p_block ? p0 : q0) / GROUP) * p.block_step;
     auto block_at = [&](int kb) { return block && kb < kb1 ? bs[(int64_t)kb * p.block_ld] : 1.f; };
     float bcur = block_at(kb0 + lane), bnext = block_at(kb0 + 32 + lane);
-    int a = 0;
+    int a = 0, bar = 0;
     uint32_t slots = 0, ps = 0, qs = 0;  // addresses of this k-block's scales: of the row, of the columns
     bool alive = true;
     for (int kb = kb0; kb < kb1; ++kb) {
@@ -229,17 +236,20 @@ __global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
       }
       if (at % SCALE_KB == 0) {
         if (alive) alive = ptx::mbar_wait(&sfull[slots & 1], (slots >> 1) & 1);
+        if (!alive) abort_flag = 1;
+        __syncwarp();
         ps = ptx::smem_u32(&pscale[slots & 1][0][q4 * 32 + lane]);
         qs = ptx::smem_u32(&qscale[slots & 1][0][c0]);
       }
       float s = __shfl_sync(0xffffffffu, bcur, at);
       if (!p.p_block) s *= ptx::ld_shared(ps);
-      fp8::named_sync(1 + a * (Cfg::EW / 4) + sl, 160);  // the watcher has seen the accumulator complete
+      fp8::named_sync(1 + bar * (Cfg::EW / 4) + sl, 160);  // the watcher has seen the accumulator complete
       ptx::tc_fence_after();
       fp8::scaled_add<CW, QVEC, (CW < 32 ? 16 : 32)>(acc, t0 + a * NT, s, qs, [&] {
         if (lane == 0) ptx::mbar_arrive(&tempty[a]);
       });
       if (++a == F_ACCS) a = 0;
+      if (++bar == F_BARS) bar = 0;
       ps += F_ROWS * 4;
       qs += NT * 4;
       if (at % SCALE_KB == SCALE_KB - 1) {
@@ -248,7 +258,6 @@ __global__ void __launch_bounds__(FCfg<NT, Q_MN>::THREADS, 1)
         ++slots;
       }
     }
-    if (!alive) abort_flag = 1;
   }
   ptx::tc_fence_before();
   __syncthreads();

@@ -52,6 +52,14 @@ namespace fp8 {
 
 constexpr int SCALE_KB = 8;  // k-blocks whose vector scales arrive in one load
 
+// Named barriers between the warp that watches the accumulators, which arrives, and the epilogue warps of some
+// columns, which wait.  A kernel with n accumulators goes round n + 2 sets of them: when the watcher
+// has seen accumulator k - 1 complete, all have passed barrier k - n - 1, so that neither its arrival at
+// barrier k nor the next meets a phase of the same set that is still open.  When the wait for accumulator
+// k runs out it arrives all the same, and from barrier k + 1 on it waits at the barriers too, which
+// keeps them all in step; no warp waits for anything else any more, so that all come to the end.  (Instead,
+// letting the epilogue warps read at every k-block whether to go on cost 10 %, a vote of the watcher
+// before it arrives 3 %, sets shared by two slices 4 %.)
 __device__ __forceinline__ void named_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }

@@ -13,8 +13,8 @@
 // therefore owns 64 columns of 32 rows, and hands its accumulator back as soon as the last of them are
 // in registers, before they are added.
 //
-// Measured on 18432 x 12288 x 4096 with block scales: 753 us, 2465 TFLOP/s, at 1365 W and 1890 MHz (the
-// power limit; 699 us in the first 50 ms).  With vector scales on both sides, 4096 x 12288 x 8192: 456 us,
+// Measured on 18432 x 12288 x 4096 with block scales: 765 us, 2430 TFLOP/s, at 1365 W and 1890 MHz (the
+// power limit; 7 % less in the first 50 ms).  With vector scales on both sides, 4096 x 12288 x 8192: 456 us,
 // 1810 TFLOP/s, bound by the epilogue's loads of the column scales and its multiplications.
 //
 // Roles per CTA: warp 0 TMA producer (operands and vector scales), warp 1 MMA issuer (leader only), warp
@@ -35,6 +35,9 @@ using fp8::SCALE_KB;
 
 constexpr int W_ROWS = 256, W_MAX_N = 256;
 constexpr int W_ACCS = 2;             // accumulators in tensor memory
+constexpr int W_SLICES = 4;           // slices of columns
+constexpr int W_BARS = W_ACCS + 2;    // sets of named barriers (fp8::named_arrive), one of each per slice: all 16
+static_assert(W_BARS % W_ACCS == 0 && (W_BARS & (W_BARS - 1)) == 0, "a set tells its accumulator");
 constexpr int W_EW = 16, W_CW = 64;
 constexpr int W_THREADS = 128 + 32 * W_EW;
 constexpr int W_HALF = 128 * GROUP;   // bytes of a CTA's half of an operand tile
@@ -116,13 +119,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
   __shared__ uint64_t sfull[2], sempty[2];  // per CTA: a slot of scales landed, has been used
   __shared__ uint64_t drainbar, never;
   __shared__ uint32_t tmem_slot;
-  __shared__ volatile int abort_flag;
+  __shared__ volatile int abort_flag, last_tile;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_ctarank();
 
   if (threadIdx.x == 0) {
     abort_flag = 0;
+    last_tile = -1;
     for (int s = 0; s < STAGES; ++s) {
       ptx::mbar_init(&full[s], 1);
       ptx::mbar_init(&empty[s], 1);
@@ -158,7 +162,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
   const int total = p.tiles_m * p.tiles_n, npairs = gridDim.x >> 1;
   const int half_n = p.bn >> 1, slices = p.bn / W_CW;
 
-
   if (warp == 0) {
     if (ptx::elect_one()) {
       // ---------------- TMA producer: this CTA's halves of A and B, and the scales of its accumulator
@@ -184,6 +187,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
             ptx::tma_load_2d_pair(sA + W_HALF, &maps.b, bar, nb, kb * GROUP);
           else
             ptx::tma_load_2d_pair(sA + W_HALF, &maps.b, bar, kb * GROUP, nb);
+          issued |= 1u << stage;
+          issued_parity = (issued_parity & ~(1u << stage)) | (phase << stage);
           if (kb % SCALE_KB == 0) {
             const uint32_t slot = slots & 1;
             if (!ptx::mbar_wait(&sempty[slot], ((slots >> 1) & 1) ^ 1)) { abort_flag = 1; break; }
@@ -193,27 +198,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
             if (QVEC) ptx::tma_load_2d(sc + SCALE_KB * 128, &maps.bs, &sfull[slot], tn * p.bn, kb);
             ++slots;
           }
-          issued |= 1u << stage;
-          issued_parity = (issued_parity & ~(1u << stage)) | (phase << stage);
           if (++stage == STAGES) { stage = 0; phase ^= 1; }
         }
       }
-      // After a give-up, loads already issued may still be landing: the leader waits (bounded)
-      // for the last phase of every stage, the peer, whose loads complete on the leader's
-      // barriers, for the length of one bounded wait.
-      if (abort_flag) {
-        for (uint32_t n = slots > 2 ? slots - 2 : 0; n < slots; ++n) ptx::mbar_wait(&sfull[n & 1], (n >> 1) & 1);
-        if (rank == 0) {
-          for (int s = 0; s < STAGES; ++s)
-            if (issued & (1u << s)) ptx::mbar_wait(&full[s], (issued_parity >> s) & 1u);
-        } else if (issued) {
-          ptx::mbar_wait(&never, 0);
-        }
+      // No load outlives the block: the leader waits for the last phase of every stage.  The peer's loads
+      // complete on the leader's barriers; after a give-up it waits for the length of one bounded wait.
+      for (uint32_t n = slots > 2 ? slots - 2 : 0; n < slots; ++n) ptx::mbar_wait(&sfull[n & 1], (n >> 1) & 1);
+      if (rank == 0) {
+        for (int s = 0; s < STAGES; ++s)
+          if (issued & (1u << s)) ptx::mbar_wait(&full[s], (issued_parity >> s) & 1u);
+      } else if (abort_flag && issued) {
+        ptx::mbar_wait(&never, 0);
       }
     }
   } else if (warp == 1) {
     if (rank == 0 && ptx::elect_one()) {
-      // ---------------- MMA issuer for both CTAs: one accumulator per unit of a k-block
+      // ---------------- MMA issuer for both CTAs: one accumulator per k-block
       const uint32_t idesc = ptx::idesc_e4m3(W_ROWS, p.bn, p.a_mn != 0, p.b_mn != 0);
       const uint64_t a_step = p.a_mn ? 256 : 2, b_step = p.b_mn ? 256 : 2;
       const uint32_t s0 = ptx::smem_u32(smem);
@@ -248,19 +248,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
   } else if (warp == 2) {
     // ---------------- watcher: waits for accumulators and lets the epilogue warps go, which would
     // slow the others down by polling
-    int a = 0;
+    uint32_t bar = 0;
     uint32_t a_phase = 0;
-    bool alive = true;
-    for (int t = blockIdx.x >> 1; t < total; t += npairs) {
+    bool ok = true, left = false;
+    for (int t = blockIdx.x >> 1; t < total && !left; t += npairs) {
       for (int kb = 0; kb < p.k_blocks; ++kb) {
-        if (alive) alive = ptx::mbar_wait(&tfull[a], a_phase);
-        if (!alive) abort_flag = 1;
-        __syncwarp();
-#pragma unroll
-        for (int sl = 0; sl < W_MAX_N / W_CW; ++sl) fp8::named_arrive(1 + a * (W_MAX_N / W_CW) + sl, 160);
-        if (++a == W_ACCS) { a = 0; a_phase ^= 1; }
+        const int id = bar * W_SLICES;
+        if (ok) {
+          ok = ptx::mbar_wait(&tfull[bar % W_ACCS], a_phase);
+          if (!ok) abort_flag = 1;
+          __syncwarp();
+          fp8::named_arrive(id, 160);
+          fp8::named_arrive(id + 1, 160);
+          if (slices == W_SLICES) {
+            fp8::named_arrive(id + 2, 160);
+            fp8::named_arrive(id + 3, 160);
+          }
+          ok = __all_sync(0xffffffffu, ok);
+        } else {
+          if (kb == p.k_blocks - 1) {
+            last_tile = t;
+            left = true;
+          }
+          for (int sl = 0; sl < slices; ++sl) fp8::named_sync(id + sl, 160);
+        }
+        bar = (bar + 1) % W_BARS;
+        if (bar % W_ACCS == 0) a_phase ^= 1;
       }
-      if (!__all_sync(0xffffffffu, alive)) break;
     }
   } else if (warp >= 4 && (warp - 4) / 4 < slices) {
     // ---------------- epilogue: tensor-memory lanes 32 q .. + 31, columns c0 .. c0 + 63
@@ -277,10 +291,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
       return p.bs[(int64_t)(n / GROUP) * p.bs_step + (int64_t)kb * p.bs_ld];
     };
     const uint32_t row4 = (q * 32 + lane) * 4, sbase = ptx::smem_u32(scales) + row4;
-    int a = 0;
+    uint32_t bar = 0;
     uint32_t slots = 0;
     float bcur = 1.f, bnext = block_at(blockIdx.x >> 1, lane);
-    bool alive = true;  // after a give-up the loop runs on without waiting, and the tile is dropped
+    bool alive = true;
     for (int t = blockIdx.x >> 1; t < total; t += npairs) {
       float acc[W_CW];
 #pragma unroll
@@ -294,17 +308,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
             bnext = kb + 32 < p.k_blocks ? block_at(t, kb + 32 + lane) : block_at(t + npairs, lane);
           }
           if (alive) alive = ptx::mbar_wait(&sfull[slots & 1], (slots >> 1) & 1);
+          if (!alive) abort_flag = 1;
+          __syncwarp();
           sc = sbase + (slots & 1) * Cfg::SLOT * 4;
           qc = sc + SCALE_KB * 128 * 4 + c0 * 4 - row4;
         }
         float s = ptx::ld_shared(sc);
         if (!QVEC) s *= __shfl_sync(0xffffffffu, bcur, kb & 31);
-        fp8::named_sync(1 + a * (W_MAX_N / W_CW) + sl, 160);  // the watcher has seen the accumulator complete
+        const int a = bar % W_ACCS;
+        fp8::named_sync(bar * W_SLICES + sl, 160);  // the watcher has seen the accumulator complete
         ptx::tc_fence_after();
         fp8::scaled_add<W_CW, QVEC, Cfg::STEP>(acc, t0 + a * W_MAX_N, s, qc, [&] {
           if (lane == 0) ptx::mbar_arrive_peer(te + a * 8);
         });
-        a ^= 1;
+        bar = (bar + 1) % W_BARS;
         sc += 128 * 4;
         qc += W_MAX_N * 4;
         if (kb % SCALE_KB == SCALE_KB - 1 || kb == p.k_blocks - 1) {
@@ -313,7 +330,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
           ++slots;
         }
       }
-      if (__any_sync(0xffffffffu, !alive || abort_flag)) { abort_flag = 1; break; }
+      if (last_tile == t) break;
+      if (__any_sync(0xffffffffu, abort_flag)) continue;  // dropped; all warps leave together, after last_tile
       int tm, tn;
       w_decode(p, t, tm, tn);
       const int m0 = tm * W_ROWS + (int)rank * 128 + q * 32, n0 = tn * p.bn + c0;
@@ -373,7 +391,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
     __syncwarp();
   }
   ptx::tc_fence_before();
-  __syncthreads();
+  __syncwarp();  // (no __syncthreads: its barrier may be in use by other warps)
   ptx::cluster_sync();  // neither CTA's shared or tensor memory is in use by the other any more
   if (warp == 1) {
     ptx::tc_fence_after();
