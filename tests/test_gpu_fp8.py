@@ -1,5 +1,9 @@
 """RMS norm with an 8-bit output, its backward, quantisation and the products of 8-bit operands,
 against plain 64-bit forms (fp8_reference.py, where the tolerances are derived)."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -529,6 +533,61 @@ def test_layer_on_a_side_stream_and_in_graphs():
             g.replay()
         check()
     assert jg.device_status() == 0
+
+
+def test_two_layers_at_once():
+    """Two streams with a layer each, over and over without waiting for one another: the bits of the
+    calls made alone."""
+    layers = [_layer(333, 768, 1000, 41), _layer(24, 1024, 640, 51)]
+    want = []
+    for t in layers:
+        _step(t)
+        want.append({k: t[k].clone() for k in OUT})
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in layers]
+    for _ in range(20):
+        for t, s in zip(layers, streams):
+            with torch.cuda.stream(s):
+                _step(t)
+    torch.cuda.synchronize()
+    for t, w in zip(layers, want):
+        for k in OUT:
+            assert torch.equal(t[k], w[k]), k
+    assert jg.device_status() == 0
+
+
+FIRST = """
+import torch
+import paper_2607_17572_gb300 as jg
+x, w = torch.randn(40, 512, device="cuda"), torch.randn(640, 512, device="cuda")
+(q, s), (wq, ws) = jg.fp8_buffers(40, 512, "row"), jg.fp8_buffers(640, 512, "block")
+y, dx, rstd = torch.empty(40, 640, device="cuda"), torch.empty(40, 512, device="cuda"), torch.empty(40, device="cuda")
+dw, n = torch.empty(512, device="cuda"), torch.empty(2, device="cuda")
+work = jg.alloc_bytes(jg.rms_norm_bwd_workspace_bytes(40, 512) + jg.grad_clip_workspace_bytes(1))
+def step():
+    jg.rms_norm_fp8(x, q, s, rstd=rstd)
+    jg.quantize_fp8(w, block=(wq, ws))
+    jg.gemm_fp8(q, s, wq, ws, y)
+    jg.rms_norm_bwd(x, x, rstd, dx, dweight=dw, ws=work)
+    jg.grad_clip([dx], 1.0, n, work)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    step()
+g.replay()
+torch.cuda.synchronize()
+outs = (y, dx, dw, n)
+got = [t.clone() for t in outs]
+step()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, outs)) and jg.device_status() == 0
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
 
 
 def test_many_calls_of_one_product_give_the_same_bits():
