@@ -435,9 +435,10 @@ int jagg_gemm_fp8(const jagg_gemm_fp8_desc* desc, cudaStream_t stream);
  * jagg_grad_norm writes norm to norm_out (device f32 [1]).
  * jagg_grad_clip writes {norm, coef} to norm_out (device f32 [2]) and out[i] = coef grads[i] (NULL: in
  * place; an out tensor is its gradient's own buffer or does not overlap any gradient).  Where coef
- * is 1 nothing is written in place.  No tensor may appear twice or overlap another.  A NaN or infinite
- * gradient makes the norm that: NaN leaves NaN in every output, infinity leaves 0 in every finite
- * element and NaN in the infinite ones.  An infinite max_norm clips nothing.
+ * is 1 nothing is written in place.  A tensor that is written must not overlap another, nor be
+ * listed twice (refused).  A NaN or infinite gradient makes the norm that: NaN leaves NaN in every
+ * output, infinity leaves 0 in every finite element and NaN in the infinite ones.  An infinite max_norm
+ * clips nothing.
  *   ws    device workspace of >= jagg_grad_clip_workspace_bytes(count) bytes, 8-byte aligned */
 int64_t jagg_grad_clip_workspace_bytes(int count);
 int jagg_grad_norm(const void* const* grads, const int64_t* numel, int count, int dtype, float* norm_out, void* ws,

@@ -6,6 +6,7 @@
 // next adds them in every CTA (the same order everywhere, so the same coefficient) and scales.  The
 // tensors' addresses travel as kernel parameters: nothing has to be copied to the device first, and
 // a captured graph keeps its own list.
+#include <algorithm>
 #include <vector>
 
 #include "fp8.cuh"
@@ -281,6 +282,41 @@ int run_lists(const ClipCall& c) {
   return JAGG_OK;
 }
 
+// What is written must not overlap anything else: two CTAs would scale an element twice, or read it scaled.
+int check_overlap(const char* who, const ClipCall& c, int es) {
+  struct Span {
+    uintptr_t first, last;  // bytes first .. last - 1
+    bool written;
+  };
+  std::vector<Span> v;
+  try {
+    v.reserve(c.out ? 2 * (size_t)c.count : c.count);
+  } catch (...) {
+    set_last_error("%s: out of host memory for %d tensors", who, c.count);
+    return JAGG_ERR_ARG;
+  }
+  bool sorted = true;
+  auto add = [&](const void* p, int64_t n, bool written) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    if (!v.empty() && a < v.back().first) sorted = false;
+    v.push_back({a, a + (uintptr_t)n * es, written});
+  };
+  for (int i = 0; i < c.count; ++i) {
+    if (c.numel[i] == 0) continue;
+    const bool own = !c.out || c.out[i] == c.grads[i];
+    add(c.grads[i], c.numel[i], own);
+    if (!own) add(c.out[i], c.numel[i], true);
+  }
+  if (!sorted) std::sort(v.begin(), v.end(), [](const Span& a, const Span& b) { return a.first < b.first; });
+  uintptr_t read = 0, written = 0;  // how far what came before reaches
+  for (const Span& s : v) {
+    JAGG_CHECK_ARG(s.first >= written && (!s.written || s.first >= read),
+                   "%s: a tensor that is written overlaps another (at %p)", who, reinterpret_cast<void*>(s.first));
+    (s.written ? written : read) = std::max(s.written ? written : read, s.last);
+  }
+  return JAGG_OK;
+}
+
 int run(const char* who, const ClipCall& c, int dtype, const void* ws, size_t ws_bytes) {
   JAGG_CHECK_ARG(fp8::is_dtype(dtype), "%s: bad dtype", who);
   JAGG_CHECK_ARG(c.count >= 0 && (c.count == 0 || (c.grads && c.numel)), "%s: %d tensors / null list", who, c.count);
@@ -299,6 +335,7 @@ int run(const char* who, const ClipCall& c, int dtype, const void* ws, size_t ws
     JAGG_CHECK_ARG(fp8::aligned(c.grads[i], es) && (!c.out || fp8::aligned(c.out[i], es)),
                    "%s: tensor %d is not aligned to its elements", who, i);
   }
+  if (c.clip) JAGG_TRY(check_overlap(who, c, es));
   double total = 0.0;
   for (int i = 0; i < c.count; ++i) total += (double)c.numel[i];
   const int tok = prof_start(c.stream);

@@ -125,3 +125,16 @@ def test_clip_refusals(jg, change, code, word):
 def test_clip_workspace_grows_with_the_lists(jg):
     f = jg.grad_clip_workspace_bytes
     assert f(0) == f(1) == f(1000) > 0 and f(1001) == 2 * f(1)
+
+
+@pytest.mark.parametrize("grads,out", [
+    ((FAKE, FAKE), None),                                          # the same tensor twice, in place
+    ((FAKE + 8, FAKE), None),                                      # the second ends inside the first
+    ((FAKE, FAKE + 64), (FAKE + 64, FAKE + 128)),                  # an output over another gradient
+    ((FAKE, FAKE + 64), (FAKE + 8, FAKE + 64)),                    # over its own gradient, shifted
+    ((FAKE, FAKE + 64), (FAKE + 128, FAKE + 136))])                # over another output
+def test_clip_of_overlapping_tensors(jg, grads, out):
+    P = ctypes.c_void_p * 2
+    st = jg.lib().jagg_grad_clip(P(*grads), P(*out) if out else None, (ctypes.c_int64 * 2)(4, 4), 2, 0, 1.0, 1e-6, FAKE, FAKE,
+                                 1 << 20, None)
+    _refused(jg, st, -1, "jagg_grad_clip", "overlap")

@@ -127,6 +127,22 @@ def test_more_than_2_31_elements():
         assert (part.cpu() == want).all()
 
 
+def test_neighbouring_and_shared_inputs():
+    """Tensors that touch are not an overlap, in any order, nor is an input that is only read listed twice;
+    the norm counts such an input twice."""
+    buf = torch.randn(3000, device="cuda", generator=torch.Generator(device="cuda").manual_seed(5))
+    parts = [buf[1000:2500], buf[:1000], buf[2500:]]
+    before, norm = buf.clone(), buf.double().norm().item()
+    out, ws = torch.empty(2, device="cuda"), _ws(3)
+    jg.grad_clip(parts, 1.0, out, ws)
+    assert abs(out[0].item() / norm - 1) <= 20 * U
+    assert torch.equal(buf, before * out[1])
+    outs = [torch.empty_like(before) for _ in range(2)]
+    jg.grad_clip([before, before], 1.0, out, ws, out=outs)
+    assert abs(out[0].item() / (2**0.5 * norm) - 1) <= 20 * U
+    assert all(torch.equal(o, before * out[1]) for o in outs)
+
+
 def test_clip_to_zero_and_no_tensors():
     _, ts = _tensors([100, 9000], torch.float32)
     out, ws = torch.empty(2, device="cuda"), _ws(2)
