@@ -340,7 +340,9 @@ int grad_reduce(const float* a, const float* b, int64_t P, float alpha, float* a
  *   column groups 128 x 1     scale[(r / 128) * lds + c]            lds >= cols
  *   blocks        128 x 128   scale[(r / 128) * lds + c / 128]      lds >= ceil(cols / 128)
  * The library writes scale = max(amax / 448, 2^-126), amax the largest magnitude of the group and
- * 448 the largest e4m3 value, and q = e4m3(x / scale), rounded to nearest even.  A group of zeros
+ * 448 the largest e4m3 value, and q = e4m3(x r), rounded to nearest even, with r = 1 / scale: quotient,
+ * reciprocal and product rounded to f32.  So q is e4m3(x / scale) but for an element whose quotient
+ * lies within 2^-23 of itself of a border between two codes, which may get either.  A group of zeros
  * stands for zeros exactly.  A group that holds a NaN or an infinity stands for NaN throughout.
  * Codes are read and written inside [rows, cols] only: what lies between cols and ldq is left
  * alone.  q must be 16-byte aligned with ldq a multiple of 16, scales of row and column groups

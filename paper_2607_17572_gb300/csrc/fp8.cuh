@@ -16,11 +16,18 @@ __device__ __forceinline__ float amax(float a, float v) {
   return m;
 }
 // The scale of a group: the largest magnitude maps to 448.  The floor 2^-126 keeps the scale and its
-// reciprocal normal numbers; a NaN or an infinity is kept (and makes every code of the group NaN).
+// reciprocal normal numbers.  A NaN is kept, and makes every code of the group NaN; so is an infinity, whose
+// reciprocal 0 makes the code of a finite element 0 and of an infinite one NaN, and times which all are NaN.
 __device__ __forceinline__ float scale_of(float a) {
   const float s = a / TOP;
   return s < 1.17549435e-38f ? 1.17549435e-38f : s;
 }
+// Elements are multiplied by the scale's reciprocal (`inv` below), rounded to f32.  On bf16 inputs, whose quotient by
+// the scale often lies next to a border between two codes, one code in 900 is the other neighbour of
+// that border than the exact quotient's, and one in 770 when the quotient is rounded to f32 instead; what
+// the codes stand for is as near to the inputs (relative 2-norm 0.025719 each).  The quotient to the bit, from the
+// product and its remainder, took 4608 x 4096 in row and column groups from 17.1 to 22.0 us.
+//
 // Two codes, `lo` in the low byte.  Rounds to nearest even; magnitudes over 448 (the group's largest
 // element times a reciprocal that was rounded up) become 448, NaN stays NaN.
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
