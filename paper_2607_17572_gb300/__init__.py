@@ -533,7 +533,7 @@ def fp8_buffers(rows: int, cols: int, form: str, device="cuda"):
     ([ceil(rows / 128), cols]) or "block" ([ceil(rows / 128), ceil(cols / 128)])."""
     shape = {"row": (_groups(cols), rows), "col": (_groups(rows), cols), "block": (_groups(rows), _groups(cols))}[form]
     q = torch.empty(rows, -(-cols // 16) * 16, dtype=torch.float8_e4m3fn, device=device)[:, :cols]
-    return q, torch.empty(shape[0], -(-shape[1] // 4) * 4, device=device)[:, :shape[1]]
+    return q, torch.empty(shape[0], -(-shape[1] // 4) * 4, dtype=_F32, device=device)[:, :shape[1]]
 
 
 def rms_norm_fp8(x, q, scale, residual=None, weight=None, eps: float = 1e-6, h_out=None, rstd=None, stream=None):
