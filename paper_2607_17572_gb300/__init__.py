@@ -478,10 +478,12 @@ def _pitch(t, dev: int, rows: int, cols: int, what: str) -> int:
     ld, one = t.stride()
     if one != 1 and cols > 1:
         raise JaggError(f"{what}: the elements of a row must be contiguous")
+    if rows == 1:
+        return (cols + 15) & ~15  # a single row's stride says nothing: a pitch that suits every operand
     if ld < cols:
         if rows > 1:
             raise JaggError(f"{what}: rows overlap (pitch {ld} below {cols})")
-        return cols  # the stride of a single row says nothing
+        return cols
     return ld
 
 
@@ -503,17 +505,14 @@ def _codes(q, dev: int, rows: int, cols: int, what: str):
     """(address, row pitch) of 8-bit codes."""
     if q.dtype not in _FP8:
         raise JaggError(f"{what} is {q.dtype}: float8_e4m3fn or uint8 expected")
-    ld = _pitch(q, dev, rows, cols, what)
-    # a single row's pitch is free: the next multiple of 16
-    return q.data_ptr(), (ld + 15) & ~15 if rows == 1 else ld
+    return q.data_ptr(), _pitch(q, dev, rows, cols, what)
 
 
 def _scales(s, dev: int, rows: int, cols: int, what: str):
-    """(address, pitch) of scales; a single row's pitch is free: the next multiple of 4."""
+    """(address, pitch) of scales."""
     if s.dtype != _F32:
         raise JaggError(f"{what} are {s.dtype}: float32 expected")
-    ld = _pitch(s, dev, rows, cols, what)
-    return s.data_ptr(), (ld + 3) & ~3 if rows == 1 else ld
+    return s.data_ptr(), _pitch(s, dev, rows, cols, what)
 
 
 def _work(ws, dev: int):

@@ -25,3 +25,30 @@ def test_scales_are_f32_whatever_the_default_dtype(default_bfloat16, form):
     assert q.dtype == torch.float8_e4m3fn and s.dtype == torch.float32
     x = torch.empty(300, 200)
     _reaches_the_device_check(jg.quantize_fp8, x, **{form: (q, s)})
+
+
+def _row(wide, cols, dtype=torch.float32):
+    """A matrix of one row, cut out of wider ones."""
+    return torch.zeros(3, wide, dtype=dtype)[1:2, :cols]
+
+
+@pytest.mark.parametrize("d", [64, 65])
+def test_the_pitch_of_a_single_row_says_nothing(d):
+    q, s = jg.fp8_buffers(1, d, "row", "cpu")
+    x = torch.zeros(1, d)
+    _reaches_the_device_check(jg.rms_norm_fp8, x, q, s, residual=_row(200, d), h_out=_row(300, d))
+    _reaches_the_device_check(jg.rms_norm_fp8, x, q, s, residual=torch.zeros(1, d), h_out=_row(300, d))
+    _reaches_the_device_check(jg.rms_norm_bwd, x, _row(100, d), torch.zeros(1), torch.zeros(1, d), dh=_row(101, d))
+    _reaches_the_device_check(jg.gemm_fp8, torch.zeros(2, 70, dtype=torch.uint8)[1:, :64], torch.zeros(1, 1),
+                              *jg.fp8_buffers(d, 64, "block", "cpu"), _row(131, d))
+
+
+def test_the_pitches_of_several_rows_have_to_agree():
+    q, s = jg.fp8_buffers(2, 64, "row", "cpu")
+    x, wide = torch.zeros(2, 64), torch.zeros(2, 80)[:, :64]
+    with pytest.raises(jg.JaggError, match="pitch"):
+        jg.rms_norm_fp8(x, q, s, residual=x, h_out=wide)
+    with pytest.raises(jg.JaggError, match="pitch"):
+        jg.rms_norm_bwd(x, x, torch.zeros(2), x, dh=wide)
+    with pytest.raises(jg.JaggError, match="overlap"):
+        jg.rms_norm_fp8(torch.zeros(64).expand(2, 64), q, s)
