@@ -609,13 +609,10 @@ def _fp8_desc(a, a_scale, b, b_scale, c, a_trans, b_trans, bias, accumulate, dev
     gk = _groups(K)
     ap, lda = _codes(a, dev, K, M, "a") if a_trans else _codes(a, dev, M, K, "a")
     bp, ldb = _codes(b, dev, K, N, "b") if b_trans else _codes(b, dev, N, K, "b")
-    block = b_scale.shape != (gk, N)
-    if not block:
-        sp, lds = _scales(b_scale, dev, gk, N, "b_scale")
-    elif b_trans:
-        sp, lds = _scales(b_scale, dev, gk, _groups(N), "b_scale")
-    else:
-        sp, lds = _scales(b_scale, dev, _groups(N), gk, "b_scale")
+    # where the forms have one shape (N = 1), they are the same addresses, and blocks need no alignment
+    form = (gk, _groups(N)) if b_trans else (_groups(N), gk)
+    block = b_scale.shape == form
+    sp, lds = _scales(b_scale, dev, *(form if block else (gk, N)), "b_scale")
     cp, cd, ldc = _mat(c, dev, M, N, "c")
     d = GemmFp8Desc(M, N, K, ap, lda, *_scales(a_scale, dev, gk, M, "a_scale"), bp, ldb, sp, lds, cp, ldc, None,
                     a_trans, b_trans, block, cd, DTYPE_F32, accumulate)

@@ -5,7 +5,7 @@ its d terms and for each of the few operations around it, relative to the sum of
 import pytest
 import torch
 
-from fp8_reference import U
+from fp8_reference import U, check_product
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,24 @@ def test_a_single_row_cut_out_of_wider_ones(d):
         buf, c1 = _cut(torch.zeros(1, N, device="cuda").to(dtype), N + 9)
         jg.gemm_fp8(q, s, *b, c1)
         assert torch.equal(c1, c) and _alone(buf, N)
+
+
+@pytest.mark.parametrize("M", [1, 5, 300])
+@pytest.mark.parametrize("K", [100, 700])
+@pytest.mark.parametrize("b_trans", [False, True])
+def test_block_scales_of_a_single_column(b_trans, K, M):
+    """Scales off 16 bytes and without a pitch of their own: the product of the aligned ones."""
+    shape = (K, 1) if b_trans else (1, K)
+    a, b = jg.fp8_buffers(M, K, "row"), jg.fp8_buffers(*shape, "block")
+    jg.quantize_fp8(_rand(M, K, seed=1), row=a)
+    jg.quantize_fp8(_rand(*shape, seed=2), block=b)
+    g = -(-K // 128)
+    off = torch.empty(g + 1, device="cuda")[1:].view(b[1].shape)
+    off.copy_(b[1])
+    c, c1 = torch.empty(M, 1, device="cuda"), torch.empty(M, 1, device="cuda")
+    jg.gemm_fp8(*a, *b, c, b_trans=b_trans)
+    jg.gemm_fp8(*a, b[0], off, c1, b_trans=b_trans)
+    assert torch.equal(c, c1)
+    va = a[0].double() * a[1].double().t().repeat_interleave(128, 1)[:, :K]
+    vb = (b[0].double().flatten() * b[1].double().flatten().repeat_interleave(128)[:K])[None]
+    check_product(c, va, vb)
