@@ -20,7 +20,6 @@
 // Roles: warp 0 TMA producer, warp 1 MMA issuer, warp 2 watches the accumulators' barriers for the
 // epilogue warps (which would slow each other down by polling), warps 4 and up the epilogue
 // (tensor-memory lanes 32 (warp % 4) .. + 31, 64 or fewer columns); all warps join and store.
-#include <atomic>
 #include <cmath>
 
 #include "../../include/jagg_testing.h"
@@ -418,11 +417,8 @@ double us_pair(int bn, bool qvec) { return bn == 256 ? (qvec ? 0.67 : 0.44) : qv
 
 // CTAs that run at one time in clusters of n: a cluster has to fit into the SMs of one GPC, so that up
 // to an eighth of the machine stays idle (18 tiles split 8 ways, 144 CTAs, take two turns: 15.6 us,
-// against 6.9 split 4 ways).  Asked once per size; all instances take an SM each.
-int cluster_ctas(int n, int* ctas) {
-  static std::atomic<int> known[F_MAX_SPLITS + 1];
-  *ctas = known[n].load(std::memory_order_relaxed);
-  if (*ctas > 0) return JAGG_OK;
+// against 6.9 split 4 ways).  Asked once per size and device; all instances take an SM each.
+int ask_cluster_ctas(int n, int* ctas) {
   auto kernel = gemm_fp8_kernel<128, false, false, false>;
   using Cfg = FCfg<128, false>;
   static OncePerDevice once;
@@ -440,14 +436,19 @@ int cluster_ctas(int n, int* ctas) {
   int clusters = 0;
   JAGG_CUDA_TRY(cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg));
   *ctas = clusters > 0 ? clusters * n : n;
-  known[n].store(*ctas, std::memory_order_relaxed);
   return JAGG_OK;
+}
+int cluster_ctas(int dev, int n, int* ctas) {
+  static NumberPerDevice known[F_MAX_SPLITS + 1];
+  return known[n].get(dev, ctas, [&](int* found) { return ask_cluster_ctas(n, found); });
 }
 
 int plan_of(const GemmFp8Args& g, Fp8Plan* plan) {
   const int kb = ceil_div(g.K, GROUP), sms = sm_count();
   int room[F_MAX_SPLITS + 1] = {0, sms};
-  for (int s = 2; s <= F_MAX_SPLITS; ++s) JAGG_TRY(cluster_ctas(s, &room[s]));
+  int dev = 0;
+  JAGG_CUDA_TRY(cudaGetDevice(&dev));
+  for (int s = 2; s <= F_MAX_SPLITS; ++s) JAGG_TRY(cluster_ctas(dev, s, &room[s]));
   Fp8Plan& best = *plan;
   double least = 0.0;
   auto offer = [&](const Fp8Plan& p, double us) {

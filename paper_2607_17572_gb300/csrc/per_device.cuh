@@ -26,4 +26,31 @@ class OncePerDevice {
   std::atomic<uint64_t> done_{0};
 };
 
+// Keeps a positive number that a call has found for each device.  Safe with several threads (two may
+// both make the call).  Devices past the 64th make it every time.
+class NumberPerDevice {
+ public:
+  // f(&number) returns its status, whose zero value is success; *number is written on success.
+  template <class F>
+  auto get(int device, int* number, F&& f) -> decltype(f(number)) {
+    using Status = decltype(f(number));
+    std::atomic<int>* at = device >= 0 && device < 64 ? &known_[device] : nullptr;
+    const int known = at ? at->load(std::memory_order_relaxed) : 0;
+    if (known > 0) {
+      *number = known;
+      return Status{};
+    }
+    int found = 0;
+    const Status st = f(&found);
+    if (st == Status{}) {
+      *number = found;
+      if (at) at->store(found, std::memory_order_relaxed);
+    }
+    return st;
+  }
+
+ private:
+  std::atomic<int> known_[64] = {};
+};
+
 }  // namespace jagg
