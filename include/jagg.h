@@ -360,8 +360,9 @@ int grad_reduce(const float* a, const float* b, int64_t P, float alpha, float* a
  *   q, scale  device, row groups of [rows, d]
  *   rstd      device [rows] f32, 1 / sqrt(mean(h^2) + eps), or NULL
  * 1 <= d <= 32768.  x, residual and h_out need the alignment of their elements only; with 16-byte
- * aligned rows and d a multiple of 8 a faster kernel runs.  A row whose sum of squares leaves f32's
- * range has 1 / sqrt 0, and zeros in q; one of zeros needs eps > 0.  */
+ * aligned rows and d a multiple of 8 a faster kernel runs.  A row whose sum of squares is above f32's
+ * range has 1 / sqrt 0, and zeros in q.  Squares below 2^-126 lose bits, which shows with eps = 0; a row
+ * whose squares are all zero needs eps > 0.  */
 int jagg_rms_norm_fp8(const void* x, int x_dtype, int64_t ldx, const void* residual, int h_dtype, int64_t ldh,
                       const void* weight, int w_dtype, int64_t rows, int64_t d, float eps, void* h_out, uint8_t* q,
                       int64_t ldq, float* scale, int64_t lds, float* rstd, cudaStream_t stream);
@@ -370,6 +371,7 @@ int jagg_rms_norm_fp8(const void* x, int x_dtype, int64_t ldx, const void* resid
  * xhat = h rstd and g = dy weight:
  *   dx      = dh + rstd (g - xhat mean(g xhat))     the gradient of x and of the residual
  *   dweight = sum over rows of dy xhat              (+= when accumulate != 0)
+ * 1 <= d <= 32768.  With 16-byte aligned rows and d a multiple of 8 up to 8192 a faster kernel runs.
  *   dy    device [rows, d] dy_dtype, row pitch lddy   gradient of y
  *   h     device [rows, d] h_dtype, row pitch ldh     as stored by the forward pass
  *   dh    device [rows, d] h_dtype, row pitch ldg, or NULL: the gradient that reaches h directly
@@ -407,7 +409,7 @@ int jagg_quantize_fp8(const void* x, int x_dtype, int64_t ldx, int64_t rows, int
  * input's gradient (A = dY, b_trans = 1), and dY, X with column groups give the weight's gradient
  * (a_trans = b_trans = 1, M = out, N = in, K = tokens) without a transposed copy.
  * Each group of 128 along K is summed by the tensor cores in f32, scaled, and added in f32.  The
- * product of two scales must be finite.
+ * product of two scales is formed in f32: it must be finite, and loses bits below 2^-126.
  *   C     device [M, N] c_dtype, row pitch ldc, aligned to its elements; accumulate != 0 adds to
  *         it (f32 only)
  *   bias  device [N] bias_dtype or NULL                                                  */

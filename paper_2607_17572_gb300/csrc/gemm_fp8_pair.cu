@@ -7,15 +7,18 @@
 // both, and each CTA's tensor memory holds its 128 rows of the accumulator.
 //
 // Per k-block of a tile of 256 columns an SM's tensor core works 512 clocks.  Meanwhile its epilogue
-// has to read 128 x 256 f32 from tensor memory and to add them, 256 clocks of f32 arithmetic and about
-// 400 in all, and hand the accumulator back: two accumulators of 256 columns fill tensor memory, so while
-// one is added the other is all that the tensor core has to work on.  Each of 16 epilogue warps
-// therefore owns 64 columns of 32 rows, and hands its accumulator back as soon as the last of them are
-// in registers, before they are added.
+// has to read 128 x 256 f32 from tensor memory and to add them, 256 clocks of f32 arithmetic, and hand the
+// accumulator back: two accumulators of 256 columns fill tensor memory, so while one is added the other
+// is all that the tensor core has to work on.  Each of 16 epilogue warps therefore owns 64 columns of 32
+// rows, and hands its accumulator back as soon as the last of them are in registers, before they are
+// added.
 //
-// Measured on 18432 x 12288 x 4096 with block scales: 765 us, 2430 TFLOP/s, at 1365 W and 1890 MHz (the
-// power limit; 7 % less in the first 50 ms).  With vector scales on both sides, 4096 x 12288 x 8192: 456 us,
-// 1810 TFLOP/s, bound by the epilogue's loads of the column scales and its multiplications.
+// Measured on 18432 x 12288 x 4096 with block scales: 772 us on the GPU (777 to 805 a call), 2400 TFLOP/s, at 1365 W and
+// 1890 MHz (the power limit; 7 % less in the first 50 ms).  That is 46 turns of 32 k-blocks of about 980 clocks, and
+// the tensor pipe is 51 to 61 % active: the epilogue's step, not the tensor core, sets the pace.  It issues
+// about 530 instructions per scheduler and k-block (54 % of the slots), of which the paired additions and
+// the loads of four warps are some 150; what the others are has not been counted.  With vector scales on both
+// sides, 4096 x 12288 x 8192: 456 us, 1810 TFLOP/s: a load and a multiplication per pair of columns more.
 //
 // Roles per CTA: warp 0 TMA producer (operands and vector scales), warp 1 MMA issuer (leader only), warp
 // 2 watches the accumulators' barriers for the epilogue warps (16 warps that poll slow down those

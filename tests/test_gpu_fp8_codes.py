@@ -100,3 +100,20 @@ def test_norm_codes(rows, d, x, h):
     _check(out.float() * rstd[:, None] * w, q, s, "row")
     jg.rms_norm_fp8(xs, q, s, residual=r, weight=w * 1e-33, rstd=rstd)
     _check(out.float() * rstd[:, None] * (w * 1e-33), q, s, "row")
+
+
+@pytest.mark.parametrize("d", [512, 333])
+def test_rows_whose_squares_leave_f32(d):
+    """Finite rows above the range of the sum: 1 / rms is 0, and so are the codes.  Small rows with eps = 0: as any
+    other while their squares are normal numbers."""
+    x = torch.randn(3, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(7))
+    x[0] *= 1e25
+    x[1] *= 1e-15
+    q, s = jg.fp8_buffers(3, d, "row")
+    rstd = torch.empty(3, device="cuda")
+    jg.rms_norm_fp8(x, q, s, eps=0.0, rstd=rstd)
+    assert rstd[0] == 0 and (q[0].float() == 0).all()
+    ref = x[1:].double().pow(2).mean(1).pow(-0.5)
+    # d terms and the shuffles, halved by the square root, the mean, the root and the reciprocal: u each
+    assert ((rstd[1:].double() - ref).abs() <= (d / 2 + 40) * 2.0 ** -24 * ref).all()
+    _check(x * rstd[:, None], q, s, "row")
